@@ -46,7 +46,8 @@ typedef enum {
   MMSP_ERR_INVALID_ARG = 1,        /* null pointer, bad range, bad divisibility            */
   MMSP_ERR_UNSUPPORTED = 2,        /* head_dim / dtype combination with no kernel          */
   MMSP_ERR_WORKSPACE_TOO_SMALL = 3,
-  MMSP_ERR_DEVICE = 4              /* launch failed; text in mmsp_last_error()             */
+  MMSP_ERR_DEVICE = 4,             /* launch failed; text in mmsp_last_error()             */
+  MMSP_ERR_NO_PAGES = 5            /* a page pool has fewer free pages than asked for      */
 } mmsp_status;
 
 /* Which (query row, key row) pairs of a block are visible.  "Position" is the index of a
@@ -260,6 +261,141 @@ mmsp_status mmsp_attn_step_bwd_static(const mmsp_shape* shape, const mmsp_block*
                                       const float* lse_final, float* delta, int compute_delta,
                                       float* dq_acc, float* dk, float* dv, int accumulate_dkdv,
                                       void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Inference: rotary positions, a paged key-value cache, and the attention of new tokens over it
+ * (Sec. 4.3, the inference mode: prefill and decoding under the same sequence parallelism).
+ * ------------------------------------------------------------------------------------------- */
+
+/* Rotary positions with several axes (video tokens have a time, a height and a width; text
+ * tokens have the same position on every axis).  Pair i of a head is (x[i], x[i + d/2]),
+ * 0 <= i < d/2, and is turned by the angle positions[axis[i]][row] * theta^(-2i/d).
+ * turns[i] is the pair's revolutions per position in units of 2^-64, so that a position times it, modulo
+ * 2^64, is the angle without rounding for any int32 position.  Filled by mmsp_rotary_plan; a caller with
+ * another rule (scaled frequencies, interleaved axes) may write turns[] and axis[] itself. */
+typedef struct {
+  int32_t head_dim;          /* 64 or 128                                                  */
+  int32_t n_axes;            /* 1 .. 4; every axis[i] < n_axes                             */
+  uint64_t turns[64];        /* head_dim / 2 used                                          */
+  uint8_t axis[64];
+} mmsp_rotary;
+
+/* Pairs are given to the axes in order, sections[a] (host, n_axes ints >= 0) to axis a.  INVALID_ARG
+ * unless theta is finite and >= 1, n_axes is in [1, 4] and the sections sum to head_dim / 2;
+ * UNSUPPORTED for a head_dim other than 64 or 128. */
+mmsp_status mmsp_rotary_plan(int32_t head_dim, double theta, int32_t n_axes, const int32_t* sections, mmsp_rotary* rotary);
+
+/* The heads of one tensor [rows, n_heads, d], element strides. */
+typedef struct {
+  void* data;                /* device, 16-byte aligned                                    */
+  int32_t n_heads;
+  int32_t dtype;             /* mmsp_dtype                                                 */
+  int64_t tok_stride, head_stride;   /* >= head_dim, multiples of 8                        */
+} mmsp_heads;
+
+/* y[t] = x[t] turned, for rows [0, n_rows) of n_tensors (1 or 2: Q and K) tensors with the same number
+ * of heads on both sides.  positions (device, int32, may be negative): position of row r on axis a at
+ * [a * pos_stride + r].  inverse != 0 turns back, which is the gradient of the forward: dX from dY.
+ * The arithmetic is fp32 and rounded once.  dtypes: both sides the same, or f32 to bf16 (gradients); the tensors
+ * of a call have the same pair of types.  y[t] may be x[t] itself (same data, strides and dtype);
+ * other overlaps are the caller's to avoid. */
+mmsp_status mmsp_rotary_apply(const mmsp_rotary* rotary, int64_t n_rows, const int32_t* positions, int64_t pos_stride,
+                              int32_t n_tensors, const mmsp_heads* x, const mmsp_heads* y, int inverse, void* hip_stream);
+
+/* A paged cache, as one call sees it: the pool of one layer and the sequences of a batch.
+ * Token c of sequence s lies in page page_table[s][c / page_size], slot c % page_size.  An entry
+ * outside [0, n_pages) is a page that is not in this pool (it lies on another rank, or was dropped): its tokens are
+ * neither read nor written here.  The attention of several ranks over their own pages is joined by
+ * mmsp_attn_merge.  Entries behind a sequence's last token are of no account.
+ * New tokens: rows [cu_new[s], cu_new[s+1]) of Q (and of K, V in mmsp_cache_append) are the last tokens of
+ * sequence s, that is row cu_new[s] + i is its token lengths[s] - n_new + i.  cu_new == NULL: one new
+ * token each, n_rows == n_seqs.  Rows from cu_new[n_seqs] on are padding and stay as they are.  A row whose token number is
+ * negative sees nothing and is not written to the cache.  Lengths beyond max_pages * page_size count as that
+ * many.  page_table, lengths and cu_new are read by the kernels, so a captured graph follows their contents. */
+typedef struct {
+  void* k; void* v;          /* device, 16-byte aligned: [n_pages][..] in io_dtype         */
+  int64_t page_stride, tok_stride, head_stride;   /* elements, of K and of V; >= head_dim, multiples of 8 */
+  int32_t n_pages;
+  int32_t page_size;         /* tokens; a positive multiple of 16                          */
+  const int32_t* page_table; /* device, [n_seqs][max_pages]                                */
+  int64_t table_stride;      /* elements between rows of page_table, >= max_pages          */
+  int32_t max_pages;         /* max_pages * page_size <= 2^30                              */
+  int32_t n_seqs;
+  const int32_t* lengths;    /* device, [n_seqs]: tokens of a sequence, its new ones included */
+  const int32_t* cu_new;     /* device, [n_seqs + 1], ascending, or NULL                   */
+  int32_t n_rows;            /* rows that the row buffers have, <= 2^30                    */
+} mmsp_cache;
+
+/* New tokens into the cache: K turned by the rotary positions (rotary == NULL: as it is) and V are
+ * written to their slots, and q_out (may be NULL, or q) receives Q turned, in one launch.  q / q_out:
+ * [n_rows, n_q_heads, d] with the shape's q strides; k, v: [n_rows, n_kv_heads, d] with its kv strides.
+ * Positions as in mmsp_rotary_apply; they need not be the token numbers.  No two rows may share a slot. */
+mmsp_status mmsp_cache_append(const mmsp_shape* shape, const mmsp_cache* cache, const mmsp_rotary* rotary,
+                              const int32_t* positions, int64_t pos_stride,
+                              const void* q, const void* k, const void* v, void* q_out, void* hip_stream);
+
+/* Bytes of device workspace mmsp_cache_attn needs for these shapes (partial results of sequences that
+ * several workgroups share; depends on n_rows, n_seqs, heads and the capacity, not on device contents). */
+size_t mmsp_cache_workspace_bytes(const mmsp_shape* shape, const mmsp_cache* cache);
+
+/* Attention of the new tokens over the cache (which mmsp_cache_append has put them into): for every row
+ * and query head
+ *   S_j = softmax_scale * Q . K[token j]  over the tokens j <= the row's own whose page is in this pool,
+ *   LSE = ln sum_j exp(S_j),  O = sum_j exp(S_j - LSE) V[token j].
+ * A row that sees nothing, or only scores of -inf, gets O = 0, LSE = -inf; one with a NaN among its scores gets NaNs.  What lies in masked slots,
+ * NaN or infinity included, has no influence.
+ * q: [n_rows, n_q_heads, d] with the shape's q strides (its kv strides are not used).  Results, each may be NULL, not
+ * all: o_final dense [n_rows, n_q_heads, d] in io_dtype; o the same in f32, for mmsp_attn_merge; lse
+ * [n_q_heads][lse_head_stride].  Meant for one or a few new tokens per sequence (any number is right; a
+ * whole prompt is faster through mmsp_attn_step_fwd).  Results are bit-identical from run to run on one kind of device.
+ * workspace: at least mmsp_cache_workspace_bytes() bytes, 16-byte aligned; its contents need not be set and
+ * nothing in it outlives the call's kernels.  Calls that may overlap in time need one each. */
+mmsp_status mmsp_cache_attn(const mmsp_shape* shape, const mmsp_cache* cache, const void* q, void* o_final, float* o,
+                            float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One page copy: tokens [0, n_tokens) of page dst become those of page src. */
+typedef struct { int32_t src, dst, n_tokens; } mmsp_page_copy;
+
+/* Page copies in the pools of n_layers layers (layer l at k + l * layer_stride, v + l * layer_stride elements), K and V,
+ * in one launch.  copies: device.  No dst may occur twice or also be a src (the plans below see to that).  An
+ * entry with an id outside [0, n_pages) or src == dst does nothing; n_tokens counts as at most page_size.  Of the shape n_kv_heads,
+ * head_dim and io_dtype are used, of the cache the pool (k, v, strides, n_pages, page_size).
+ * layer_stride: a multiple of 8 (any if n_layers == 1). */
+mmsp_status mmsp_cache_copy_pages(const mmsp_shape* shape, const mmsp_cache* cache, int32_t n_layers, int64_t layer_stride,
+                                  const mmsp_page_copy* copies, int32_t n_copies, void* hip_stream);
+
+/* Which pages of a pool are in use, by how many sequences.  Host integers in the caller's arrays; one pool
+ * serves all layers.  Not synchronised: one thread at a time. */
+typedef struct {
+  int32_t n_pages, page_size;
+  int32_t* refs;             /* host, [n_pages]: sequences that hold the page              */
+  int32_t* free_pages;       /* host, [n_pages]: the first n_free are free, the last of them is given out next */
+  int32_t n_free;
+} mmsp_pages;
+
+/* All pages free, given out in ascending order.  n_pages, page_size, refs and free_pages must be set. */
+mmsp_status mmsp_pages_init(mmsp_pages* pages);
+
+/* Room for tokens [n_old, n_new) of the sequence whose page table row (host, max_pages entries) is `row`.
+ * If its last page is partly filled and other sequences hold it too, this sequence gets a page of its own
+ * and *copy receives the copy that mmsp_cache_copy_pages has to make before the new tokens are written; *n_copies receives 0 or 1.
+ * NO_PAGES if the pool has too few free pages.  A call that fails changes nothing, here and below. */
+mmsp_status mmsp_pages_grow(mmsp_pages* pages, int32_t* row, int32_t max_pages, int64_t n_old, int64_t n_new,
+                            mmsp_page_copy* copy, int32_t* n_copies);
+
+/* new_row becomes a second sequence with the pages of row's first n_tokens tokens, all shared. */
+mmsp_status mmsp_pages_fork(mmsp_pages* pages, const int32_t* row, int32_t max_pages, int64_t n_tokens, int32_t* new_row);
+
+/* The sequence lets go of its pages; those that nobody else holds are free.  Its entries become -1. */
+mmsp_status mmsp_pages_free(mmsp_pages* pages, int32_t* row, int32_t max_pages, int64_t n_tokens);
+
+/* Moves the pages in use to the front of the pool, so that pages [*n_used, n_pages) are all free: pages behind
+ * that border move into the holes before it, each in the order of its ids, no other page moves.  rows: the page table
+ * rows (host, row_stride apart) of ALL sequences of the pool, n_tokens their lengths (host); entries are rewritten.
+ * copies (host, room for n_pages) receives *n_copies copies for mmsp_cache_copy_pages.  INVALID_ARG if the rows and refs
+ * do not agree. */
+mmsp_status mmsp_pages_compact(mmsp_pages* pages, int32_t* rows, int64_t row_stride, int32_t max_pages, int32_t n_seqs,
+                               const int64_t* n_tokens, mmsp_page_copy* copies, int32_t* n_copies, int32_t* n_used);
 
 /* Message for the last non-OK status returned on the calling thread ("" if none). */
 const char* mmsp_last_error(void);

@@ -12,13 +12,15 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmmsp.so")
 
-MMSP_OK, MMSP_ERR_INVALID_ARG, MMSP_ERR_UNSUPPORTED, MMSP_ERR_WORKSPACE_TOO_SMALL, MMSP_ERR_DEVICE = range(5)
+MMSP_OK, MMSP_ERR_INVALID_ARG, MMSP_ERR_UNSUPPORTED, MMSP_ERR_WORKSPACE_TOO_SMALL, MMSP_ERR_DEVICE, MMSP_ERR_NO_PAGES = range(6)
 MMSP_MASK_FULL, MMSP_MASK_CAUSAL_DIAG, MMSP_MASK_NONE = 0, 1, 2
 MMSP_BF16, MMSP_F32 = 0, 1
 
 EXPORTS = ["mmsp_zigzag_layout", "mmsp_zigzag_plan", "mmsp_contiguous_plan", "mmsp_zigzag_plan_packed", "mmsp_2d_layout", "mmsp_workspace_bytes", "mmsp_attn_step_fwd",
            "mmsp_attn_merge", "mmsp_attn_delta", "mmsp_attn_step_bwd", "mmsp_attn_step_bwd_static", "mmsp_zigzag_gather", "mmsp_zigzag_scatter",
-           "mmsp_a2a_pack_heads", "mmsp_a2a_unpack_heads", "mmsp_last_error"]
+           "mmsp_a2a_pack_heads", "mmsp_a2a_unpack_heads", "mmsp_rotary_plan", "mmsp_rotary_apply", "mmsp_cache_append", "mmsp_cache_workspace_bytes",
+           "mmsp_cache_attn", "mmsp_cache_copy_pages", "mmsp_pages_init", "mmsp_pages_grow", "mmsp_pages_fork", "mmsp_pages_free", "mmsp_pages_compact",
+           "mmsp_last_error"]
 
 
 class MmspShape(ctypes.Structure):
@@ -39,6 +41,31 @@ class Mmsp2dShare(ctypes.Structure):
     _fields_ = [("head_rank", ctypes.c_int32), ("ring_rank", ctypes.c_int32), ("q_head0", ctypes.c_int32),
                 ("n_q_heads", ctypes.c_int32), ("kv_head0", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("chunk_ids", ctypes.c_int32 * 2), ("chunk_len", ctypes.c_int64)]
+
+
+class MmspRotary(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("turns", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+class MmspHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class MmspCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("page_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("lengths", ctypes.c_void_p),
+                ("cu_new", ctypes.c_void_p), ("n_rows", ctypes.c_int32)]
+
+
+class MmspPageCopy(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_int32), ("dst", ctypes.c_int32), ("n_tokens", ctypes.c_int32)]
+
+
+class MmspPages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("refs", ctypes.POINTER(ctypes.c_int32)),
+                ("free_pages", ctypes.POINTER(ctypes.c_int32)), ("n_free", ctypes.c_int32)]
 
 
 class MmspError(RuntimeError):
@@ -75,8 +102,22 @@ _lib.mmsp_attn_step_bwd.argtypes = [ctypes.POINTER(MmspShape), ctypes.POINTER(Mm
                                     _INT, _P, _P, _P, _INT, _P, _SZ, _P]
 _lib.mmsp_attn_step_bwd_static.argtypes = [ctypes.POINTER(MmspShape), ctypes.POINTER(MmspBlock), _P, _P, _P, _P, _P, _P,
                                            _P, _INT, _P, _P, _P, _INT, _P]
+_ROT, _HEADS, _CACHE, _PAGES, _IP = (ctypes.POINTER(x) for x in (MmspRotary, MmspHeads, MmspCache, MmspPages, _I32))
+_COPY = ctypes.POINTER(MmspPageCopy)
+_lib.mmsp_rotary_plan.argtypes = [_I32, ctypes.c_double, _I32, _IP, _ROT]
+_lib.mmsp_rotary_apply.argtypes = [_ROT, _I64, _P, _I64, _I32, _HEADS, _HEADS, _INT, _P]
+_lib.mmsp_cache_append.argtypes = [ctypes.POINTER(MmspShape), _CACHE, _ROT, _P, _I64, _P, _P, _P, _P, _P]
+_lib.mmsp_cache_workspace_bytes.restype = _SZ
+_lib.mmsp_cache_workspace_bytes.argtypes = [ctypes.POINTER(MmspShape), _CACHE]
+_lib.mmsp_cache_attn.argtypes = [ctypes.POINTER(MmspShape), _CACHE, _P, _P, _P, _P, _P, _SZ, _P]
+_lib.mmsp_cache_copy_pages.argtypes = [ctypes.POINTER(MmspShape), _CACHE, _I32, _I64, _P, _I32, _P]
+_lib.mmsp_pages_init.argtypes = [_PAGES]
+_lib.mmsp_pages_grow.argtypes = [_PAGES, _IP, _I32, _I64, _I64, _COPY, _IP]
+_lib.mmsp_pages_fork.argtypes = [_PAGES, _IP, _I32, _I64, _IP]
+_lib.mmsp_pages_free.argtypes = [_PAGES, _IP, _I32, _I64]
+_lib.mmsp_pages_compact.argtypes = [_PAGES, _IP, _I64, _I32, _I32, ctypes.POINTER(_I64), _COPY, _IP, _IP]
 for _name in EXPORTS:
-    if _name not in ("mmsp_last_error", "mmsp_workspace_bytes"):
+    if _name not in ("mmsp_last_error", "mmsp_workspace_bytes", "mmsp_cache_workspace_bytes"):
         getattr(_lib, _name).restype = _INT
 
 
@@ -197,3 +238,91 @@ def mmsp_attn_step_bwd(shape, blk, q, k, v, o_final, d_o, lse_final, delta, comp
                                    _ptr(d_o), _ptr(lse_final), _ptr(delta), int(compute_delta), _ptr(dq_acc),
                                    _ptr(dk), _ptr(dv), int(accumulate_dkdv), _ptr(workspace), workspace_bytes,
                                    stream or None))
+
+
+# ---- inference: rotary positions, the paged cache ----
+
+def make_heads(data, n_heads, dtype, tok_stride, head_stride):
+    return MmspHeads(_ptr(data), n_heads, dtype, tok_stride, head_stride)
+
+
+def make_cache(k, v, strides, n_pages, page_size, page_table=None, table_stride=0, max_pages=0, n_seqs=0, lengths=None, cu_new=None, n_rows=0):
+    """strides = (page, token, head) in elements, of K and of V."""
+    return MmspCache(_ptr(k), _ptr(v), strides[0], strides[1], strides[2], n_pages, page_size, _ptr(page_table), table_stride, max_pages, n_seqs,
+                     _ptr(lengths), _ptr(cu_new), n_rows)
+
+
+def mmsp_rotary_plan(head_dim, theta, sections):
+    rotary = MmspRotary()
+    _check(_lib.mmsp_rotary_plan(head_dim, theta, len(sections), (_I32 * len(sections))(*sections), ctypes.byref(rotary)))
+    return rotary
+
+
+def mmsp_rotary_apply(rotary, n_rows, positions, pos_stride, x, y, inverse=False, stream=0):
+    """x, y: one or two MmspHeads each."""
+    if len(x) != len(y):
+        raise ValueError("%d tensors to turn, %d to write" % (len(x), len(y)))
+    _check(_lib.mmsp_rotary_apply(ctypes.byref(rotary), n_rows, _ptr(positions), pos_stride, len(x), (MmspHeads * len(x))(*x),
+                                  (MmspHeads * len(y))(*y), int(inverse), stream or None))
+
+
+def mmsp_cache_append(shape, cache, rotary, positions, pos_stride, q, k, v, q_out=None, stream=0):
+    _check(_lib.mmsp_cache_append(ctypes.byref(shape), ctypes.byref(cache), None if rotary is None else ctypes.byref(rotary), _ptr(positions),
+                                  pos_stride, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), stream or None))
+
+
+def mmsp_cache_workspace_bytes(shape, cache):
+    return _lib.mmsp_cache_workspace_bytes(ctypes.byref(shape), ctypes.byref(cache))
+
+
+def mmsp_cache_attn(shape, cache, q, o_final, o, lse, workspace=None, workspace_bytes=0, stream=0):
+    _check(_lib.mmsp_cache_attn(ctypes.byref(shape), ctypes.byref(cache), _ptr(q), _ptr(o_final), _ptr(o), _ptr(lse), _ptr(workspace),
+                                workspace_bytes, stream or None))
+
+
+def mmsp_cache_copy_pages(shape, cache, n_layers, layer_stride, copies, n_copies, stream=0):
+    """copies: device int32 tensor [n_copies, 3] of (src, dst, n_tokens)."""
+    _check(_lib.mmsp_cache_copy_pages(ctypes.byref(shape), ctypes.byref(cache), n_layers, layer_stride, _ptr(copies), n_copies, stream or None))
+
+
+def _host(a, kind, dtype, what):
+    """Pointer to a numpy array's data; only the very type and layout the call reads is taken."""
+    if not isinstance(a, np.ndarray) or a.dtype != dtype or not a.flags.c_contiguous:
+        raise ValueError("%s must be a C-contiguous numpy array of %s" % (what, np.dtype(dtype).name))
+    return a.ctypes.data_as(ctypes.POINTER(kind))
+
+
+def make_pages(refs, free_pages, page_size):
+    """Bookkeeping in two numpy int32 arrays of n_pages, which the caller keeps."""
+    if len(refs) != len(free_pages):
+        raise ValueError("refs and free_pages must have one entry for each page")
+    pages = MmspPages(len(refs), page_size, _host(refs, _I32, np.int32, "refs"), _host(free_pages, _I32, np.int32, "free_pages"), 0)
+    _check(_lib.mmsp_pages_init(ctypes.byref(pages)))
+    return pages
+
+
+def mmsp_pages_grow(pages, row, n_old, n_new):
+    """Returns the page copy to make, (src, dst, n_tokens), or None."""
+    copy, n = MmspPageCopy(), _I32()
+    _check(_lib.mmsp_pages_grow(ctypes.byref(pages), _host(row, _I32, np.int32, "row"), len(row), n_old, n_new, ctypes.byref(copy), ctypes.byref(n)))
+    return (copy.src, copy.dst, copy.n_tokens) if n.value else None
+
+
+def mmsp_pages_fork(pages, row, n_tokens, new_row):
+    if len(new_row) < len(row):
+        raise ValueError("new_row has %d entries, row %d" % (len(new_row), len(row)))
+    _check(_lib.mmsp_pages_fork(ctypes.byref(pages), _host(row, _I32, np.int32, "row"), len(row), n_tokens, _host(new_row, _I32, np.int32, "new_row")))
+
+
+def mmsp_pages_free(pages, row, n_tokens):
+    _check(_lib.mmsp_pages_free(ctypes.byref(pages), _host(row, _I32, np.int32, "row"), len(row), n_tokens))
+
+
+def mmsp_pages_compact(pages, rows, n_tokens):
+    """rows [n_seqs, max_pages], n_tokens [n_seqs] (int64).  Returns (copies [n, 3] int32, pages in use)."""
+    if rows.ndim != 2 or len(rows) != len(n_tokens):
+        raise ValueError("one row and one length for each sequence")
+    copies, n, used = np.zeros((pages.n_pages, 3), dtype=np.int32), _I32(), _I32()
+    _check(_lib.mmsp_pages_compact(ctypes.byref(pages), _host(rows, _I32, np.int32, "rows"), rows.shape[1], rows.shape[1], len(rows),
+                                   _host(n_tokens, _I64, np.int64, "n_tokens"), copies.ctypes.data_as(_COPY), ctypes.byref(n), ctypes.byref(used)))
+    return copies[:n.value], used.value

@@ -6,12 +6,12 @@
 #include <cstring>
 #include <mutex>
 
-#include "../../include/mmsp.h"
+#include "api_checks.h"
 #include "common.h"
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
+namespace mmsp {
 
 mmsp_status fail(mmsp_status st, const char* fmt, ...) {
   va_list ap;
@@ -20,10 +20,6 @@ mmsp_status fail(mmsp_status st, const char* fmt, ...) {
   va_end(ap);
   return st;
 }
-
-constexpr int64_t kMaxExtent = (int64_t)1 << 30;   // rows and positions are int32 inside the kernels
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 mmsp_status check_shape(const mmsp_shape* s) {
   if (s == nullptr) return fail(MMSP_ERR_INVALID_ARG, "shape is NULL");
@@ -47,6 +43,17 @@ mmsp_status check_shape(const mmsp_shape* s) {
   if (s->lse_head_stride < 0) return fail(MMSP_ERR_INVALID_ARG, "lse_head_stride is negative");
   return MMSP_OK;
 }
+
+mmsp_status device_result(hipError_t e, const char* what) {
+  if (e == hipSuccess) return MMSP_OK;
+  return fail(MMSP_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+}  // namespace mmsp
+
+using namespace mmsp;
+
+namespace {
 
 mmsp_status check_rows(const mmsp_shape* s, int64_t row0, int64_t n_rows) {
   if (row0 < 0 || n_rows < 0 || row0 + n_rows > kMaxExtent)
@@ -88,11 +95,6 @@ mmsp::StepArgs make_args(const mmsp_shape* s, const mmsp_block* b) {
   if (a.mask == MMSP_MASK_CAUSAL_DIAG && b->q_pos0 >= b->k_pos0 + b->n_k - 1) a.mask = MMSP_MASK_FULL;   // no key follows the first query
   a.n_docs = b->n_docs; a.cu = b->cu_seqlens;
   return a;
-}
-
-mmsp_status device_result(hipError_t e, const char* what) {
-  if (e == hipSuccess) return MMSP_OK;
-  return fail(MMSP_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
 // Only the bf16 backward needs scratch: padded row statistics and partial dQ, dK and dV of work that was

@@ -1,0 +1,499 @@
+// Attention of new tokens over a paged key-value cache: every K and V row is read once for the handful of query rows that
+// share its KV head, so the memory rate bounds it (28/4 heads, one token: 7 of the 16 columns of a matrix instruction, 3.5 flops a byte).
+//
+// Work.  The (token, head) pairs of a KV head's new rows are one list, as in the forward kernel; groups of kRows of it are
+// stationary.  A pair of (sequence, KV head, group) has ceil(length / 128) tiles of 128 keys.  The tiles of all pairs are one sequence that is cut
+// into as many equal ranges as there are workgroups, whatever the lengths are: a workgroup goes through the segments
+// of pairs in its range.  A pair inside one range is finished there; at most the first and the last segment of a range are
+// parts of pairs that others share: their (O, maximum, sum) goes to the workspace and a second launch joins them.  The lengths are on the device only,
+// so each workgroup adds up the tiles of all sequences for itself.
+//
+// Wavefronts.  The four wavefronts of a workgroup take different keys and meet when a segment ends, so the loop has no barrier and
+// no LDS.  S^T = K . Q^T: K rows are A operands as they lie in memory.  O^T += V^T . P^T: the 16 keys of a block are dealt to the contraction
+// slots so that the accumulators of S^T are B operands as they are, and a lane's V pieces (8 elements of d of the 8 keys of its
+// slots, each row read as 256 contiguous bytes by 16 lanes) become the A operands of 8 products by exchanging halves of registers.
+#include <algorithm>
+#include <type_traits>
+
+#include "mfma_tiles.h"
+#include "paged.h"
+
+namespace mmsp {
+namespace {
+
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+
+constexpr int kTile = 128;                              // keys of a tile
+constexpr int kWaves = 4;
+
+struct Partial {
+  int64_t* prefix;                                      // [n_seqs + 1] tiles of the sequences before
+  float* m; float* l;                                   // [2 W][kRows]
+  float* o;                                             // [2 W][kRows][d]
+};
+
+// Groups of kRows rows of a KV head's list, and tiles of each of their pairs.
+struct PairShape { int groups, tiles; };
+template <int kRows>
+__device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const SeqRows& r) {
+  PairShape p;
+  p.groups = (int)(((int64_t)r.count * a.group + kRows - 1) / kRows);
+  p.tiles = max(1, (r.length + kTile - 1) / kTile);     // rows that see nothing have a tile too: someone has to say so
+  return p;
+}
+
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// Range of workgroup w of n: [total * w / n, total * (w + 1) / n).  The workgroup that tile t falls to:
+__device__ __forceinline__ int64_t range_begin(int64_t total, int w, int n) { return total * w / n; }
+__device__ __forceinline__ int range_of(int64_t total, int64_t t, int n) { return (int)(((t + 1) * n - 1) / total); }
+
+template <bool kBf16, int kD, int kNT>
+__global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a, int n_groups, Partial part) {
+  constexpr int kRows = 16 * kNT, kElt = kBf16 ? 2 : 4;
+  constexpr int kBlocks = kBf16 ? 2 : 1, kKeys = 16 * kBlocks;   // blocks of 16 keys, keys of a step
+  constexpr int kKL = kD * kElt / 64;                   // 16-byte pieces of a K row that a lane holds
+  constexpr int kVC = kD * kElt / 256;                  // .. of a V row
+  constexpr int kAcc = kD / 16;                         // O^T accumulators of 16 rows of d
+  constexpr int kPad = kD + 4;
+  __shared__ float red[kWaves][16][kPad];
+  __shared__ float red_m[kWaves][kRows], red_l[kWaves][kRows];
+  __shared__ int64_t wave_tiles[kWaves];
+  __shared__ int64_t found[2];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const CacheArgs& c = a.cache;
+
+  // ---- this workgroup's range of tiles ----
+  const int per = (c.n_seqs + 255) / 256, s_first = min(tid * per, c.n_seqs), s_last = min(s_first + per, c.n_seqs);
+  auto tiles_of_seq = [&](int s) {
+    const PairShape p = pairs_of<kRows>(a, rows_of_seq(c, s));
+    return (int64_t)p.groups * a.Hkv * p.tiles;
+  };
+  int64_t mine = 0;
+  for (int s = s_first; s < s_last; ++s) mine += tiles_of_seq(s);
+  int64_t upto = mine;                                  // of the threads up to this one
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1) {
+    const int64_t x = __shfl_up(upto, w);
+    if (lane >= w) upto += x;
+  }
+  if (lane == 63) wave_tiles[wave] = upto;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) upto += wave_tiles[w];
+    total += wave_tiles[w];
+  }
+  total = uniform64(total);
+  if (blockIdx.x == 0) {                                // for the joining launch
+    int64_t x = upto - mine;
+    for (int s = s_first; s < s_last; ++s) { part.prefix[s] = x; x += tiles_of_seq(s); }
+    if (tid == 0) part.prefix[c.n_seqs] = total;
+  }
+  const int n = (int)min((int64_t)n_groups, total);     // ranges, none of them empty
+  if ((int)blockIdx.x >= n) return;
+  int64_t t = range_begin(total, blockIdx.x, n);
+  const int64_t t_end = range_begin(total, blockIdx.x + 1, n);
+  if (upto - mine <= t && t < upto) {                   // one thread
+    int64_t x = upto - mine;
+    int s = s_first;
+    for (;; ++s) {
+      const int64_t y = tiles_of_seq(s);
+      if (t < x + y) break;
+      x += y;
+    }
+    found[0] = s;
+    found[1] = x;
+  }
+  __syncthreads();
+  int seq = __builtin_amdgcn_readfirstlane((int)found[0]);
+  int64_t base = uniform64(found[1]);
+
+  const float sc = a.scale * kLog2e;
+  while (t < t_end) {
+    const SeqRows r = rows_of_seq(c, seq);
+    const PairShape shape = pairs_of<kRows>(a, r);
+    const int64_t n_seq = (int64_t)shape.groups * a.Hkv * shape.tiles;
+    if (t >= base + n_seq) { base += n_seq; ++seq; continue; }
+    const int64_t pair = (t - base) / shape.tiles;
+    const int tile0 = (int)(t - base - pair * shape.tiles);
+    const int tile1 = (int)min((int64_t)shape.tiles, tile0 + (t_end - t));
+    const int kvh = __builtin_amdgcn_readfirstlane((int)(pair / shape.groups)), group0 = (int)(pair - (int64_t)kvh * shape.groups) * kRows;
+    t += tile1 - tile0;
+
+    // ---- rows ----
+    const int n_list = r.count * a.group, first_pos = r.length - r.count;
+    int hi[kNT];                                        // last key that this lane's rows see
+    u32x4 q[kNT][kKL];
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      const int i = group0 + j * 16 + col, ic = min(i, n_list - 1);
+      const int tok = (int)((uint32_t)ic / a.group_div);
+      hi[j] = first_pos + tok;                          // a row behind the last one does as that one
+      const char* p = reinterpret_cast<const char*>(a.q) + ((int64_t)(r.first + tok) * a.q_ts + (kvh * a.group + ic - tok * a.group) * a.q_hs) * kElt + quad * 16;
+#pragma unroll
+      for (int i2 = 0; i2 < kKL; ++i2) q[j][i2] = *reinterpret_cast<const u32x4*>(p + i2 * 64);
+    }
+    const int hi_max = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)(min(group0 + kRows, n_list) - 1) / a.group_div));
+    const int hi_min = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)group0 / a.group_div));
+    const int key_end = min(tile1 * kTile, hi_max + 1);
+
+    f32x4 acc[kNT][kAcc];
+    float m[kNT], l[kNT];                               // l: of this lane's keys
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      m[j] = -INFINITY;
+      l[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kAcc; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const char* const k_head = c.k + kvh * c.head_stride * kElt;
+    const char* const v_head = c.v + kvh * c.head_stride * kElt;
+    const uint32_t k_lane = (uint32_t)(col * c.tok_stride * kElt + quad * 16), v_lane = (uint32_t)(quad * 4 * c.tok_stride * kElt + col * 16);
+    const uint32_t v_step = (uint32_t)(c.tok_stride * kElt);
+    const int32_t* const table = c.table + seq * c.table_stride;
+
+    for (int k0 = tile0 * kTile + wave * kKeys; k0 < key_end; k0 += kWaves * kKeys) {
+      // Blocks of 16 keys lie inside a page.  One that is not here, beside one that is, is read from page 0 and masked.
+      int64_t block_at[kBlocks];
+      bool here[kBlocks], any = false;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const int kb = k0 + 16 * b, p = (int)((uint32_t)kb / c.page_div);
+        const int page = kb < key_end ? load_const(table, p) : -1;
+        here[b] = page >= 0 && page < c.n_pages;
+        any = any || here[b];
+        block_at[b] = here[b] ? (page * c.page_stride + (kb - p * c.page_size) * c.tok_stride) * kElt : 0;
+      }
+      if (!any) continue;
+      u32x4 k[kBlocks][kKL], v[kBlocks][4][kVC];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const int64_t off = block_at[b];
+#pragma unroll
+        for (int i = 0; i < kKL; ++i) k[b][i] = *reinterpret_cast<const u32x4*>(k_head + off + k_lane + i * 64);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int x = 0; x < kVC; ++x) v[b][i][x] = *reinterpret_cast<const u32x4*>(v_head + off + v_lane + i * v_step + x * 256);
+      }
+      bool whole = k0 + kKeys - 1 <= hi_min;             // every row sees every key of the step
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) whole = whole && here[b];
+
+      // P^T: lane (col, quad) holds row col, keys 16 b + 4 quad + i
+      f32x4 p[kNT][kBlocks];
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+          f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < kKL; ++i) {
+            if constexpr (kBf16) {
+              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[b][i]), __builtin_bit_cast(bf16x8, q[j][i]), s, 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[b][i][e]), __uint_as_float(q[j][i][e]), s, 0, 0, 0);
+            }
+          }
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = here[b] && k0 + 16 * b + quad * 4 + i <= hi[j] ? s[i] : -INFINITY;
+          }
+          p[j][b] = s;
+        }
+        float top = p[j][0][0];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, p[j][b][i]);
+        top *= sc;
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m[j], top), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m[j] - ref);   // m = -inf: 0
+        m[j] = m_new;
+        l[j] *= alpha;
+#pragma unroll
+        for (int i = 0; i < kAcc; ++i) acc[j][i] *= alpha;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[j][b][i] = __builtin_amdgcn_exp2f(p[j][b][i] * sc - ref);
+            l[j] += p[j][b][i];
+          }
+      }
+
+      // O^T += V^T . P^T.  P goes in as two bf16 numbers, its rounding and what that leaves: 16 bits together, so that a partial result is as
+      // exact as the fp32 it is kept in; the second product costs nothing where memory sets the pace.
+      auto add_pv = [&](f32x4 (&to)[kAcc], int j) {
+        if constexpr (kBf16) {
+          uint32_t hi_w[4], lo_w[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float p0 = p[j][x >> 1][(x & 1) * 2], p1 = p[j][x >> 1][(x & 1) * 2 + 1];
+            hi_w[x] = pack2(p0, p1);
+            lo_w[x] = pack2(p0 - __uint_as_float(hi_w[x] << 16), p1 - __uint_as_float(hi_w[x] & 0xffff0000u));
+          }
+          const bf16x8 ph = __builtin_bit_cast(bf16x8, mk4(hi_w[0], hi_w[1], hi_w[2], hi_w[3])), pl = __builtin_bit_cast(bf16x8, mk4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {                  // d = 8 (row of A) + e
+            const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
+            uint32_t w[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) w[x] = __builtin_amdgcn_perm(v[x >> 1][(x & 1) * 2 + 1][0][e >> 1], v[x >> 1][(x & 1) * 2][0][e >> 1], pick);
+            const bf16x8 va = __builtin_bit_cast(bf16x8, mk4(w[0], w[1], w[2], w[3]));
+            to[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph, to[e], 0, 0, 0);
+            to[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, to[e], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < kVC; ++x)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)                // d = 64 x + 4 (row of A) + e
+                to[x * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][i][x][e]), p[j][0][i], to[x * 4 + e], 0, 0, 0);
+        }
+      };
+      bool odd = false;                                  // a key that some rows see and others do not has an infinity or NaN in V
+      if (!whole) {
+        // What no row sees is not to be multiplied, not even by zero: it may be anything.
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = k0 + 16 * b + quad * 4 + i;
+            const bool none = !here[b] || key > hi_max, some = key > hi_min;
+#pragma unroll
+            for (int x = 0; x < kVC; ++x)
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                const uint32_t word = none ? 0u : v[b][i][x][w];
+                v[b][i][x][w] = word;
+                if constexpr (kBf16) odd |= some && ((word & 0x7f80u) == 0x7f80u || (word & 0x7f800000u) == 0x7f800000u);
+                else odd |= some && (word & 0x7f800000u) == 0x7f800000u;
+              }
+          }
+      }
+      if (!__any(odd)) {
+#pragma unroll
+        for (int j = 0; j < kNT; ++j) add_pv(acc[j], j);
+      } else {                                           // token by token, the last one first: V without the keys that it does not see
+        for (int limit = hi_max; limit >= hi_max - kRows && limit >= first_pos; --limit) {
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int x = 0; x < kVC; ++x)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v[b][i][x][w] = k0 + 16 * b + quad * 4 + i > limit ? 0u : v[b][i][x][w];
+#pragma unroll
+          for (int j = 0; j < kNT; ++j) {
+            f32x4 x[kAcc];
+#pragma unroll
+            for (int i = 0; i < kAcc; ++i) x[i] = acc[j][i];
+            add_pv(x, j);
+#pragma unroll
+            for (int i = 0; i < kAcc; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[j][i][e] = hi[j] == limit ? x[i][e] : acc[j][i][e];
+          }
+        }
+      }
+    }
+
+    // ---- the wavefronts' results joined ----
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      l[j] += __shfl_xor(l[j], 16);
+      l[j] += __shfl_xor(l[j], 32);
+      if (quad == 0) {
+        red_m[wave][j * 16 + col] = m[j];
+        red_l[wave][j * 16 + col] = l[j];
+      }
+    }
+    const bool finished = tile0 == 0 && tile1 == shape.tiles;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (tile0 == 0 ? 1 : 0);
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < kAcc; e += 4) {
+          // bf16: accumulators 0..7 are 8 consecutive d; f32: 0..3 (4..7 of the upper half) are 4
+          const int d = kBf16 ? (quad * 4 + i) * 8 + e : (e / 4) * 64 + (quad * 4 + i) * 4;
+          *reinterpret_cast<f32x4*>(&red[wave][col][d]) = f32x4{acc[j][e][i], acc[j][e + 1][i], acc[j][e + 2][i], acc[j][e + 3][i]};
+        }
+      __syncthreads();
+      const int row = tid >> 4, jr = j * 16 + row;       // 16 threads share a row
+      constexpr int kEach = kD / 16;
+      float top = red_m[0][jr];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w][jr]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, x[kEach];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(red_m[w][jr] - ref);
+        sum += f * red_l[w][jr];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) x[e] += f * red[w][row][(tid & 15) * kEach + e];
+      }
+      const int i = group0 + jr;
+      if (i < n_list) {
+        if (finished) {
+          const int tok = (int)((uint32_t)i / a.group_div), h = kvh * a.group + i - tok * a.group;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          const int64_t at = ((int64_t)(r.first + tok) * a.Hq + h) * kD + (tid & 15) * kEach;
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) x[e] *= inv;
+          if (a.o != nullptr)
+#pragma unroll
+            for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(a.o + at + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+          if (a.o_final != nullptr) {
+            if constexpr (kBf16) {
+              *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.o_final) + at) = mk4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+            } else {
+#pragma unroll
+              for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.o_final) + at + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+            }
+          }
+          if (a.lse != nullptr && (tid & 15) == 0) a.lse[h * a.lse_hs + r.first + tok] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+        } else {
+          float* const to = part.o + (slot * kRows + jr) * kD + (tid & 15) * kEach;
+#pragma unroll
+          for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+          if ((tid & 15) == 0) { part.m[slot * kRows + jr] = top; part.l[slot * kRows + jr] = sum; }
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// Joins the partial results of pairs that several workgroups shared.  A workgroup takes one (row, head); teams of d / 4 threads share out the partial results.
+template <bool kBf16, int kD, int kRows>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a, int n_groups, Partial part) {
+  constexpr int kTeam = kD / 4, kTeams = 256 / kTeam;
+  __shared__ f32x4 xs[kTeams][kTeam];
+  __shared__ float ms[kTeams], ls[kTeams];
+  const CacheArgs& c = a.cache;
+  const int row = blockIdx.x / a.Hq, h = blockIdx.x - row * a.Hq;
+  const int seq = seq_of_row(c, row);
+  if (seq < 0) return;
+  const SeqRows r = rows_of_seq(c, seq);
+  const PairShape shape = pairs_of<kRows>(a, r);
+  const int kvh = (int)((uint32_t)h / a.group_div), i = (row - r.first) * a.group + h - kvh * a.group;
+  if (i < 0 || row - r.first >= r.count) return;
+  const int64_t total = part.prefix[c.n_seqs], t0 = part.prefix[seq] + ((int64_t)kvh * shape.groups + i / kRows) * shape.tiles;
+  const int n = (int)min((int64_t)n_groups, total);
+  const int w0 = range_of(total, t0, n), w1 = range_of(total, t0 + shape.tiles - 1, n), count = w1 - w0 + 1;
+  if (count == 1) return;                               // finished where it was computed
+  const int team = threadIdx.x / kTeam, e = threadIdx.x % kTeam, jr = i % kRows;
+  auto slot = [&](int s) { return 2 * (int64_t)(w0 + s) + (s == 0 ? 1 : 0); };
+  float top = -INFINITY;
+  for (int s = team; s < count; s += kTeams) top = fmaxf(top, part.m[slot(s) * kRows + jr]);
+  float ref = top == -INFINITY ? 0.f : top, sum = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = team; s < count; s += kTeams) {
+    const int64_t at = slot(s) * kRows + jr;
+    const float f = __builtin_amdgcn_exp2f(part.m[at] - ref);
+    sum += f * part.l[at];
+    x += f * *reinterpret_cast<const f32x4*>(part.o + at * kD + e * 4);
+  }
+  xs[team][e] = x;
+  if (e == 0) { ms[team] = top; ls[team] = sum; }
+  __syncthreads();
+  if (team != 0) return;
+  for (int k = 0; k < kTeams; ++k) top = fmaxf(top, ms[k]);
+  ref = top == -INFINITY ? 0.f : top;
+  sum = 0.f;
+  x = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < kTeams; ++k) {
+    const float f = __builtin_amdgcn_exp2f(ms[k] - ref);
+    sum += f * ls[k];
+    x += f * xs[k][e];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  x *= inv;
+  const int64_t at = ((int64_t)row * a.Hq + h) * kD + e * 4;
+  if (a.o != nullptr) *reinterpret_cast<f32x4*>(a.o + at) = x;
+  if (a.o_final != nullptr) {
+    if constexpr (kBf16) *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.o_final) + at) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.o_final) + at) = x;
+  }
+  if (a.lse != nullptr && e == 0) a.lse[h * a.lse_hs + row] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// How a call is laid out: tiles of 16 rows of a workgroup's group, workgroups.
+struct Plan { int nt, groups; };
+Plan plan_of(const CacheAttnArgs& a) {
+  const CacheArgs& c = a.cache;
+  // As many rows as a sequence has on average in one group, up to 64: every further group reads the keys again.
+  const int64_t mean = ((int64_t)c.n_rows * a.group + c.n_seqs - 1) / c.n_seqs;
+  Plan p;
+  p.nt = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
+  const int64_t rows = 16 * p.nt, capacity = (int64_t)c.max_pages * c.page_size;
+  const int64_t pairs = ((int64_t)c.n_rows * a.group / rows + c.n_seqs) * a.Hkv, room = (int64_t)cu_count() * (p.nt == 1 ? 2 : 1);
+  p.groups = (int)std::min(room, std::min(pairs, room) * std::max<int64_t>(1, (capacity + kTile - 1) / kTile));
+  return p;
+}
+
+int64_t align16(int64_t x) { return (x + 15) / 16 * 16; }
+
+}  // namespace
+
+int64_t cache_attn_workspace_bytes(const CacheAttnArgs& a, int io_dtype) {
+  (void)io_dtype;
+  const Plan p = plan_of(a);
+  return align16(8 * ((int64_t)a.cache.n_seqs + 1)) + (int64_t)2 * p.groups * 16 * p.nt * 4 * (2 + a.d);
+}
+
+hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t stream) {
+  if (a.cache.n_rows == 0 || a.cache.n_seqs == 0) return hipSuccess;
+  const Plan p = plan_of(a);
+  Partial part;
+  char* w = a.ws;
+  part.prefix = reinterpret_cast<int64_t*>(w);
+  w += align16(8 * ((int64_t)a.cache.n_seqs + 1));
+  const int64_t rows = (int64_t)2 * p.groups * 16 * p.nt;
+  part.o = reinterpret_cast<float*>(w);
+  part.m = part.o + rows * a.d;
+  part.l = part.m + rows;
+  auto launch = [&](auto bf16, auto d, auto nt) {
+    constexpr bool kBf16 = decltype(bf16)::value;
+    constexpr int kD = decltype(d)::value, kNT = decltype(nt)::value;
+    cache_attn_kernel<kBf16, kD, kNT><<<dim3((unsigned)p.groups), dim3(256), 0, stream>>>(a, p.groups, part);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.groups == 1) return e;
+    cache_join_kernel<kBf16, kD, 16 * kNT><<<dim3((unsigned)((int64_t)a.cache.n_rows * a.Hq)), dim3(256), 0, stream>>>(a, p.groups, part);
+    return hipGetLastError();
+  };
+  auto by_rows = [&](auto bf16, auto d) {
+    switch (p.nt) {
+      case 1: return launch(bf16, d, std::integral_constant<int, 1>());
+      case 2: return launch(bf16, d, std::integral_constant<int, 2>());
+      default: return launch(bf16, d, std::integral_constant<int, 4>());
+    }
+  };
+  if (io_dtype == 0) return by_rows(std::true_type(), std::integral_constant<int, 128>());
+  if (a.d == 128) return by_rows(std::false_type(), std::integral_constant<int, 128>());
+  return by_rows(std::false_type(), std::integral_constant<int, 64>());
+}
+
+}  // namespace mmsp
