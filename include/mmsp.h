@@ -327,8 +327,9 @@ typedef struct {
 } mmsp_cache;
 
 /* New tokens into the cache: K turned by the rotary positions (rotary == NULL: as it is) and V are
- * written to their slots, and q_out (may be NULL, or q) receives Q turned, in one launch.  q / q_out:
- * [n_rows, n_q_heads, d] with the shape's q strides; k, v: [n_rows, n_kv_heads, d] with its kv strides.
+ * written to their slots, and q_out receives Q turned, in one launch.  q: [n_rows, n_q_heads, d] with the shape's
+ * q strides; q_out: NULL (Q is left alone), q itself (in place, with q's strides), or a dense
+ * [n_rows, n_q_heads, d] that does not overlap q; k, v: [n_rows, n_kv_heads, d] with the shape's kv strides.
  * Positions as in mmsp_rotary_apply; they need not be the token numbers.  No two rows may share a slot. */
 mmsp_status mmsp_cache_append(const mmsp_shape* shape, const mmsp_cache* cache, const mmsp_rotary* rotary,
                               const int32_t* positions, int64_t pos_stride,

@@ -187,6 +187,8 @@ mmsp_status mmsp_cache_append(const mmsp_shape* shape, const mmsp_cache* cache, 
   a.cache = cache_args(cache);
   a.q = reinterpret_cast<const char*>(q); a.k = reinterpret_cast<const char*>(k); a.v = reinterpret_cast<const char*>(v); a.q_out = reinterpret_cast<char*>(q_out);
   a.q_ts = shape->q_tok_stride; a.q_hs = shape->q_head_stride; a.kv_ts = shape->kv_tok_stride; a.kv_hs = shape->kv_head_stride;
+  a.out_ts = q_out == q ? a.q_ts : (int64_t)shape->n_q_heads * shape->head_dim;
+  a.out_hs = q_out == q ? a.q_hs : shape->head_dim;
   a.Hq = q_out != nullptr ? shape->n_q_heads : 0; a.Hkv = shape->n_kv_heads;
   RotaryArgs r;
   if (rotary != nullptr) r = rotary_args(rotary, positions, pos_stride, false);

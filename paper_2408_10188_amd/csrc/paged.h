@@ -56,7 +56,7 @@ hipError_t launch_rotary(const RotaryArgs& rot, const HeadsArgs (&t)[2], int n_t
 struct AppendArgs {
   CacheArgs cache;
   const char* q; const char* k; const char* v; char* q_out;
-  int64_t q_ts, q_hs, kv_ts, kv_hs;
+  int64_t q_ts, q_hs, out_ts, out_hs, kv_ts, kv_hs;     // out: of q_out
   int32_t Hq, Hkv;                                      // Hq: 0 without q_out
 };
 hipError_t launch_append(const AppendArgs& a, const RotaryArgs* rot, int d, int io_dtype, hipStream_t stream);

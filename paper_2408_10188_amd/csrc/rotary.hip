@@ -139,9 +139,8 @@ __global__ __launch_bounds__(256) void append_kernel(RotaryArgs rot, AppendArgs 
     const char* x;
     char* y;
     if (is_q) {
-      const int64_t off = (row * a.q_ts + h * a.q_hs + piece * 8) * kBytes;
-      x = a.q + off;
-      y = a.q_out + off;
+      x = a.q + (row * a.q_ts + h * a.q_hs + piece * 8) * kBytes;
+      y = a.q_out + (row * a.out_ts + h * a.out_hs + piece * 8) * kBytes;
     } else {
       if (!here) continue;
       const int hh = h - a.Hq - (is_v ? a.Hkv : 0);

@@ -157,16 +157,18 @@ class PagedCache:
         return B.make_shape(self.n_q_heads, hkv, d, _io(self.k), scale, _strides(q), strides, q.shape[0])
 
     def append(self, layer, rotary, positions, q, k, v, q_out=None):
-        """Writes the step's K (turned by `rotary` at `positions` [n_axes, rows]) and V into `layer`'s pages; returns Q turned (into q_out,
-        of q's strides, or q itself)."""
+        """Writes the step's K (turned by `rotary` at `positions` [n_axes, rows]) and V into `layer`'s pages; returns Q turned (into q_out:
+        contiguous, or q itself, which is also what None means)."""
         import torch
         cache, n = self._cache(layer), self._step[3]
         q_out = q if q_out is None else q_out
         for t in (q, k, v, q_out):
             if t.shape[0] != n or t.dtype != self.k.dtype or t.stride(2) != 1:
                 raise ValueError("%d rows of %s with d contiguous are wanted" % (n, self.k.dtype))
-        if _strides(k) != _strides(v) or _strides(q) != _strides(q_out) or q.shape != q_out.shape or k.shape != v.shape:
-            raise ValueError("K and V, and Q and q_out, must have the same shapes and strides")
+        if _strides(k) != _strides(v) or k.shape != v.shape or q.shape != q_out.shape:
+            raise ValueError("K and V must have the same shapes and strides, q_out Q's shape")
+        if q_out.stride() != q.stride() if q_out.data_ptr() == q.data_ptr() else not q_out.is_contiguous():
+            raise ValueError("q_out must be contiguous, or q itself")
         if q.shape[1:] != (self.n_q_heads, self.k.shape[-1]) or k.shape[1:] != (self.k.shape[2], self.k.shape[-1]):
             raise ValueError("Q and K must have the cache's heads")
         if rotary is not None and (positions.dtype != torch.int32 or positions.shape != (rotary.n_axes, n) or positions.stride(1) != 1):

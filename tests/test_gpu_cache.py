@@ -232,7 +232,8 @@ def test_append(case, dtype, d, turned):
     k, v = (torch.randn(p.n_rows, 3 * p.hkv, d, device=DEV, generator=gen).to(dtype)[:, p.hkv:2 * p.hkv] for _ in range(2))
     pos = torch.randint(0, 1 << 18, (3, p.n_rows + 2), device=DEV, generator=gen, dtype=torch.int32)
     before = p.k.clone(), p.v.clone(), p.q.clone()
-    q_out = nans_like(torch.empty(p.n_rows, p.hq + 2 * p.hkv + 1, d, dtype=dtype, device=DEV))[:, :p.hq]
+    room = nans(p.n_rows + 3, p.hq, d, dtype=dtype)        # q_out is dense, Q lies in wider rows; a guard behind it
+    q_out = room[:p.n_rows]
     shape = B.make_shape(p.hq, p.hkv, d, B.MMSP_F32 if dtype == F32 else B.MMSP_BF16, 1.0, (p.q.stride(0), d), (k.stride(0), d), p.n_rows)
     rot = B.mmsp_rotary_plan(d, THETA, SECTIONS[d]) if turned else None
     B.mmsp_cache_append(shape, p.cache, rot, pos, pos.stride(0), p.q, k, v, q_out)
@@ -242,7 +243,7 @@ def test_append(case, dtype, d, turned):
         B.mmsp_rotary_apply(rot, p.n_rows, pos, pos.stride(0), [paged.heads_of(t) for t in x], [paged.heads_of(t) for t in y])
         want_q, want_k = y
     rows = p.n_rows if p.cu is None else int(p.cu[-1])
-    assert torch.equal(q_out[:rows], want_q[:rows]) and bool(torch.isnan(q_out[rows:]).all()) and torch.equal(p.q, before[2])
+    assert torch.equal(q_out[:rows], want_q[:rows]) and bool(torch.isnan(room[rows:]).all()) and torch.equal(p.q, before[2])
     host = [t.float().cpu().numpy() for t in (*before[:2], want_k, v)]
     orc.append(host[0], host[1], p.table, p.page, p.lengths, p.cu, host[2], host[3])
     for got, want in zip((p.k, p.v), host[:2]):             # every other slot as it was, NaN in the unused ones
