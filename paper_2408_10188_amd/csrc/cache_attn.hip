@@ -48,6 +48,13 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// A word of V (two bf16 numbers or one f32) with zeros in the place of infinities and NaN.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+  if constexpr (kBf16) return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+  else return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+}
+
 // Range of workgroup w of n: [total * w / n, total * (w + 1) / n).  The workgroup that tile t falls to:
 __device__ __forceinline__ int64_t range_begin(int64_t total, int w, int n) { return total * w / n; }
 __device__ __forceinline__ int range_of(int64_t total, int64_t t, int n) { return (int)(((t + 1) * n - 1) / total); }
@@ -145,6 +152,7 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
     const int hi_min = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)group0 / a.group_div));
     const int key_end = min(tile1 * kTile, hi_max + 1);
 
+    bool odd = false;                                   // this lane has left out an infinity or NaN of V
     f32x4 acc[kNT][kAcc];
     float m[kNT], l[kNT];                               // l: of this lane's keys
 #pragma unroll
@@ -161,33 +169,64 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
     const uint32_t v_step = (uint32_t)(c.tok_stride * kElt);
     const int32_t* const table = c.table + seq * c.table_stride;
 
-    for (int k0 = tile0 * kTile + wave * kKeys; k0 < key_end; k0 += kWaves * kKeys) {
-      // Blocks of 16 keys lie inside a page.  One that is not here, beside one that is, is read from page 0 and masked.
-      int64_t block_at[kBlocks];
-      bool here[kBlocks], any = false;
+    // Steps of this wavefront, kKeys keys each: step i takes keys key_of(i) .. + kKeys.  A refill looks up the pages of the next 64
+    // blocks, one a lane; steps without any page here are passed over.
+    struct Step {
+      int k0;
+      uint32_t here;                                    // bit b: block b lies in this pool
+      int64_t at[kBlocks];                              // where the blocks lie, in bytes
+    };
+    auto key_of = [&](int i) { return tile0 * kTile + (i * kWaves + wave) * kKeys; };
+    int ahead = 0, pages = 0, end = 0;                  // first step of the refill; page of this lane's block; keys end here
+    uint64_t todo = 0;                                  // blocks of the refill that are here and not fetched
+    auto refill = [&] {
+      const int kb = key_of(ahead + lane / kBlocks) + 16 * (lane % kBlocks);
+      pages = kb < end ? table[(uint32_t)kb / c.page_div] : -1;
+      todo = __ballot(pages >= 0 && pages < c.n_pages);
+    };
+    auto begin = [&](int first, int to) {
+      ahead = first;
+      end = to;
+      todo = 0;
+      if (key_of(first) < to) refill();
+    };
+    auto next = [&](Step& x) {
+      while (todo == 0) {
+        ahead += 64 / kBlocks;
+        if (key_of(ahead) >= end) return false;
+        refill();
+      }
+      const int i = __builtin_ctzll(todo) / kBlocks;
+      x.here = (uint32_t)(todo >> (i * kBlocks)) & ((1u << kBlocks) - 1);
+      todo &= ~((((uint64_t)1 << kBlocks) - 1) << (i * kBlocks));
+      x.k0 = key_of(ahead + i);
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
-        const int kb = k0 + 16 * b, p = (int)((uint32_t)kb / c.page_div);
-        const int page = kb < key_end ? load_const(table, p) : -1;
-        here[b] = page >= 0 && page < c.n_pages;
-        any = any || here[b];
-        block_at[b] = here[b] ? (page * c.page_stride + (kb - p * c.page_size) * c.tok_stride) * kElt : 0;
+        // Blocks lie inside a page.  One that is not here, beside one that is, is read from page 0 and masked.
+        const int kb = x.k0 + 16 * b, slot = kb - (int)((uint32_t)kb / c.page_div) * c.page_size, page = __builtin_amdgcn_readlane(pages, i * kBlocks + b);
+        x.at[b] = x.here >> b & 1 ? (page * c.page_stride + slot * c.tok_stride) * kElt : 0;
       }
-      if (!any) continue;
-      u32x4 k[kBlocks][kKL], v[kBlocks][4][kVC];
+      return true;
+    };
+    // Read once, past the caches: 7.1 TB/s in a large plain read where the default policy reaches 6.2.
+    u32x4 k[kBlocks][kKL], v[kBlocks][4][kVC];
+    auto load_k = [&](const Step& x) {
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        const int64_t off = block_at[b];
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < kKL; ++i) k[b][i] = *reinterpret_cast<const u32x4*>(k_head + off + k_lane + i * 64);
+        for (int e = 0; e < kKL; ++e) k[b][e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k_head + x.at[b] + k_lane + e * 64));
+    };
+    auto load_v = [&](const Step& x) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-          for (int x = 0; x < kVC; ++x) v[b][i][x] = *reinterpret_cast<const u32x4*>(v_head + off + v_lane + i * v_step + x * 256);
-      }
-      bool whole = k0 + kKeys - 1 <= hi_min;             // every row sees every key of the step
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) whole = whole && here[b];
+          for (int e = 0; e < kVC; ++e) v[b][r][e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v_head + x.at[b] + v_lane + r * v_step + e * 256));
+    };
+    // edge: the step has keys that some rows see and others do not.  Computes a step, and asks for the following one's K and V as soon as the registers that they go to are free.
+    auto compute = [&](const Step& x, auto edge, auto has_next, const Step& after) {
+      const bool whole = !decltype(edge)::value && x.k0 + kKeys - 1 <= hi_max && x.here == (1u << kBlocks) - 1;   // every row sees every key
 
       // P^T: lane (col, quad) holds row col, keys 16 b + 4 quad + i
       f32x4 p[kNT][kBlocks];
@@ -207,10 +246,14 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
           }
           if (!whole) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = here[b] && k0 + 16 * b + quad * 4 + i <= hi[j] ? s[i] : -INFINITY;
+            for (int i = 0; i < 4; ++i) s[i] = (x.here >> b & 1) && x.k0 + 16 * b + quad * 4 + i <= hi[j] ? s[i] : -INFINITY;
           }
           p[j][b] = s;
         }
+      }
+      if constexpr (decltype(has_next)::value) load_k(after);
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
         float top = p[j][0][0];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
@@ -236,81 +279,110 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
 
       // O^T += V^T . P^T.  P goes in as two bf16 numbers, its rounding and what that leaves: 16 bits together, so that a partial result is as
       // exact as the fp32 it is kept in; the second product costs nothing where memory sets the pace.
-      auto add_pv = [&](f32x4 (&to)[kAcc], int j) {
-        if constexpr (kBf16) {
+      bf16x8 p_hi[kNT], p_lo[kNT];
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int j = 0; j < kNT; ++j) {
           uint32_t hi_w[4], lo_w[4];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const float p0 = p[j][x >> 1][(x & 1) * 2], p1 = p[j][x >> 1][(x & 1) * 2 + 1];
-            hi_w[x] = pack2(p0, p1);
-            lo_w[x] = pack2(p0 - __uint_as_float(hi_w[x] << 16), p1 - __uint_as_float(hi_w[x] & 0xffff0000u));
+          for (int w = 0; w < 4; ++w) {
+            const float p0 = p[j][w >> 1][(w & 1) * 2], p1 = p[j][w >> 1][(w & 1) * 2 + 1];
+            hi_w[w] = pack2(p0, p1);
+            lo_w[w] = pack2(p0 - __uint_as_float(hi_w[w] << 16), p1 - __uint_as_float(hi_w[w] & 0xffff0000u));
           }
-          const bf16x8 ph = __builtin_bit_cast(bf16x8, mk4(hi_w[0], hi_w[1], hi_w[2], hi_w[3])), pl = __builtin_bit_cast(bf16x8, mk4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]));
+          p_hi[j] = __builtin_bit_cast(bf16x8, mk4(hi_w[0], hi_w[1], hi_w[2], hi_w[3]));
+          p_lo[j] = __builtin_bit_cast(bf16x8, mk4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]));
+        }
+      }
+      // What no row sees is not to be multiplied, not even by zero: it may be anything.  Nor is an infinity or NaN that some rows see and others do
+      // not (some_too): it is left out here and added to the rows that see it after the loop.
+      constexpr int kMasks = 4;                          // bf16: pairs of keys; f32: keys
+      uint32_t seen[kMasks], some[kMasks];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {                  // d = 8 (row of A) + e
+      for (int y = 0; y < kMasks; ++y) {
+        const int key = kBf16 ? x.k0 + 16 * (y >> 1) + quad * 4 + (y & 1) * 2 : x.k0 + quad * 4 + y;
+        const int b = kBf16 ? y >> 1 : 0;
+        const bool in = x.here >> b & 1;
+        auto bits = [](bool first, bool second) { return kBf16 ? (first ? 0xffffu : 0u) | (second ? 0xffff0000u : 0u) : first ? ~0u : 0u; };
+        seen[y] = bits(in && key <= hi_max, in && key + 1 <= hi_max);
+        some[y] = bits(key > hi_min, key + 1 > hi_min);
+      }
+      auto add_pv = [&](auto some_too) {
+        auto word = [&](uint32_t w, int y) {
+          w &= seen[y];
+          if constexpr (decltype(some_too)::value) {
+            const uint32_t left_out = (w ^ finite_part<kBf16>(w)) & some[y];
+            odd = odd || left_out != 0;
+            w ^= left_out;
+          }
+          return w;
+        };
+#pragma unroll
+        for (int e = 0; e < kAcc; ++e) {
+          bf16x8 va = {};
+          float vf[4] = {};
+          if constexpr (kBf16) {                         // d = 8 (row of A) + e
             const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
             uint32_t w[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) w[x] = __builtin_amdgcn_perm(v[x >> 1][(x & 1) * 2 + 1][0][e >> 1], v[x >> 1][(x & 1) * 2][0][e >> 1], pick);
-            const bf16x8 va = __builtin_bit_cast(bf16x8, mk4(w[0], w[1], w[2], w[3]));
-            to[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph, to[e], 0, 0, 0);
-            to[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, to[e], 0, 0, 0);
+            for (int y = 0; y < 4; ++y) w[y] = word(__builtin_amdgcn_perm(v[y >> 1][(y & 1) * 2 + 1][0][e >> 1], v[y >> 1][(y & 1) * 2][0][e >> 1], pick), y);
+            va = __builtin_bit_cast(bf16x8, mk4(w[0], w[1], w[2], w[3]));
+          } else {                                       // d = 64 (e / 4) + 4 (row of A) + e % 4
+#pragma unroll
+            for (int y = 0; y < 4; ++y) vf[y] = __uint_as_float(word(v[0][y][e / 4][e % 4], y));
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int x = 0; x < kVC; ++x)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)                // d = 64 x + 4 (row of A) + e
-                to[x * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][i][x][e]), p[j][0][i], to[x * 4 + e], 0, 0, 0);
-        }
-      };
-      bool odd = false;                                  // a key that some rows see and others do not has an infinity or NaN in V
-      if (!whole) {
-        // What no row sees is not to be multiplied, not even by zero: it may be anything.
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = k0 + 16 * b + quad * 4 + i;
-            const bool none = !here[b] || key > hi_max, some = key > hi_min;
-#pragma unroll
-            for (int x = 0; x < kVC; ++x)
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const uint32_t word = none ? 0u : v[b][i][x][w];
-                v[b][i][x][w] = word;
-                if constexpr (kBf16) odd |= some && ((word & 0x7f80u) == 0x7f80u || (word & 0x7f800000u) == 0x7f800000u);
-                else odd |= some && (word & 0x7f800000u) == 0x7f800000u;
-              }
-          }
-      }
-      if (!__any(odd)) {
-#pragma unroll
-        for (int j = 0; j < kNT; ++j) add_pv(acc[j], j);
-      } else {                                           // token by token, the last one first: V without the keys that it does not see
-        for (int limit = hi_max; limit >= hi_max - kRows && limit >= first_pos; --limit) {
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int x = 0; x < kVC; ++x)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) v[b][i][x][w] = k0 + 16 * b + quad * 4 + i > limit ? 0u : v[b][i][x][w];
 #pragma unroll
           for (int j = 0; j < kNT; ++j) {
-            f32x4 x[kAcc];
+            if constexpr (kBf16) {
+              acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_hi[j], acc[j][e], 0, 0, 0);
+              acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_lo[j], acc[j][e], 0, 0, 0);
+            } else {
 #pragma unroll
-            for (int i = 0; i < kAcc; ++i) x[i] = acc[j][i];
-            add_pv(x, j);
-#pragma unroll
-            for (int i = 0; i < kAcc; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[j][i][e] = hi[j] == limit ? x[i][e] : acc[j][i][e];
+              for (int i = 0; i < 4; ++i) acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i], p[j][0][i], acc[j][e], 0, 0, 0);
+            }
           }
         }
+      };
+      add_pv(edge);
+      if constexpr (decltype(has_next)::value) load_v(after);
+    };
+    // keys [0, edge) are seen by all rows or, from hi_max + 1 on, by none
+    const int edge = hi_min == hi_max ? key_end : min(key_end, max(0, hi_min + 1) / kKeys * kKeys);
+    Step now, after;
+    begin(0, edge);
+    if (next(now)) {
+      load_k(now);
+      load_v(now);
+      while (next(after)) {
+        compute(now, std::false_type(), std::true_type(), after);
+        now = after;
+      }
+      compute(now, std::false_type(), std::false_type(), now);
+    }
+    if (edge < key_end) {
+      begin(max(0, edge - tile0 * kTile + (kWaves - 1 - wave) * kKeys) / (kWaves * kKeys), key_end);   // the first step with keys from `edge` on
+      while (next(now)) {
+        load_k(now);
+        load_v(now);
+        compute(now, std::true_type(), std::false_type(), now);
+      }
+    }
+    if (__any(odd)) {
+      for (int key = max(tile0 * kTile, hi_min + 1); key < key_end; ++key) {
+        const int tp = (int)((uint32_t)key / c.page_div), page = table[tp];
+        if (page < 0 || page >= c.n_pages) continue;
+        const char* const row = v_head + (page * c.page_stride + (key - tp * c.page_size) * c.tok_stride) * kElt;
+#pragma unroll
+        for (int e = 0; e < kAcc; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x;
+            if constexpr (kBf16) x = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[(quad * 4 + i) * 8 + e] << 16);
+            else x = reinterpret_cast<const float*>(row)[(e / 4) * 64 + (quad * 4 + i) * 4 + e % 4];
+            const bool counts = !(fabsf(x) < INFINITY);
+#pragma unroll
+            for (int j = 0; j < kNT; ++j) acc[j][e][i] += counts && key <= hi[j] ? x : 0.f;
+          }
       }
     }
 
