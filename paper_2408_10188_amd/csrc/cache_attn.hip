@@ -23,8 +23,20 @@ namespace {
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
-constexpr int kTile = 128;                              // keys of a tile
-constexpr int kWaves = 4;
+#ifndef WR
+#define WR 4
+#endif
+constexpr int kWholeRounds = WR;
+#ifndef JB
+#define JB 4
+#endif
+#ifndef JO
+#define JO 8
+#endif
+// Wavefronts of a workgroup: two on each SIMD, or one with all of its registers where there are more than 16 rows.
+template <int kNT> constexpr int waves_of() { return kNT == 1 ? 8 : 4; }
+constexpr int kRound = 32;                              // keys of a tile: a multiple of this times the wavefronts
+constexpr int kMaxGroups = 1024;                        // workgroups of a launch
 
 struct Partial {
   int64_t* prefix;                                      // [n_seqs + 1] tiles of the sequences before
@@ -35,11 +47,31 @@ struct Partial {
 // Groups of kRows rows of a KV head's list, and tiles of each of their pairs.
 struct PairShape { int groups, tiles; };
 template <int kRows>
-__device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const SeqRows& r) {
+__device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const SeqRows& r, const FastDiv& tile) {
   PairShape p;
   p.groups = (int)(((int64_t)r.count * a.group + kRows - 1) / kRows);
-  p.tiles = max(1, (r.length + kTile - 1) / kTile);     // rows that see nothing have a tile too: someone has to say so
+  p.tiles = max(1, (int)((uint32_t)(r.length + (int)tile.d - 1) / tile));   // rows that see nothing have a tile too: someone has to say so
   return p;
+}
+
+// kN numbers to `at` and on, as bf16 or fp32.
+template <bool kBf16, int kN>
+__device__ __forceinline__ void store_row(void* to, int64_t at, const float (&x)[kN]) {
+  if constexpr (kBf16) {
+    uint32_t w[kN / 2];
+#pragma unroll
+    for (int e = 0; e < kN / 2; ++e) w[e] = pack2(x[2 * e], x[2 * e + 1]);
+    uint16_t* const p = reinterpret_cast<uint16_t*>(to) + at;
+    if constexpr (kN == 8) *reinterpret_cast<u32x4*>(p) = mk4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+  } else {
+    float* const p = reinterpret_cast<float*>(to) + at;
+#pragma unroll
+    for (int e = 0; e < kN; e += kN < 4 ? 2 : 4) {
+      if constexpr (kN < 4) *reinterpret_cast<f32x2*>(p + e) = f32x2{x[e], x[e + 1]};
+      else *reinterpret_cast<f32x4*>(p + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+    }
+  }
 }
 
 // A value that is the same in all lanes, in scalar registers.
@@ -48,6 +80,17 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// Asynchronous copy of 64 x 16 bytes to LDS (see dma16), read once and so past the caches: 7.1 TB/s in a large plain read where the default policy
+// reaches 6.2.
+__device__ __forceinline__ void copy_past_caches(const char* base, uint32_t offset, const void* lds_array, int byte_offset) {
+  const uint32_t lds = lds_address(lds_array) + (uint32_t)byte_offset;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(lds), "v"(offset), "s"(base) : "memory");
+}
+// Until all but the last n copies have landed; until all LDS reads have returned.
+template <int kN>
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kN) : "memory"); }
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
 // A word of V (two bf16 numbers or one f32) with zeros in the place of infinities and NaN.
 template <bool kBf16>
 __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
@@ -55,19 +98,28 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
   else return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
 }
 
-// Range of workgroup w of n: [total * w / n, total * (w + 1) / n).  The workgroup that tile t falls to:
-__device__ __forceinline__ int64_t range_begin(int64_t total, int w, int n) { return total * w / n; }
-__device__ __forceinline__ int range_of(int64_t total, int64_t t, int n) { return (int)(((t + 1) * n - 1) / total); }
+// The quotient of numbers that almost always fit 32 bits; a 64-bit division is over a hundred dependent instructions.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  if ((uint64_t)(x | y) >> 32 == 0) return (uint32_t)x / (uint32_t)y;
+  return x / y;
+}
+// Tiles of a workgroup's range: workgroup w has tiles [w * each, (w + 1) * each) of `total`.
+__device__ __forceinline__ int64_t tiles_each(int64_t total, int n_groups) { return quotient(total + n_groups - 1, n_groups); }
 
 template <bool kBf16, int kD, int kNT>
-__global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a, int n_groups, Partial part) {
+__global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a, int n_groups, FastDiv tile, Partial part) {
+  constexpr int kWaves = waves_of<kNT>(), kThreads = 64 * kWaves;
   constexpr int kRows = 16 * kNT, kElt = kBf16 ? 2 : 4;
   constexpr int kBlocks = kBf16 ? 2 : 1, kKeys = 16 * kBlocks;   // blocks of 16 keys, keys of a step
   constexpr int kKL = kD * kElt / 64;                   // 16-byte pieces of a K row that a lane holds
   constexpr int kVC = kD * kElt / 256;                  // .. of a V row
   constexpr int kAcc = kD / 16;                         // O^T accumulators of 16 rows of d
   constexpr int kPad = kD + 4;
-  __shared__ float red[kWaves][16][kPad];
+  constexpr int kHalf = kKeys * kD * kElt, kCopies = kHalf / 1024;   // bytes of a step's K (or V), copies that bring them
+  // A wavefront's K and V of a step; when a segment ends, the wavefronts' O, [kWaves][16][kPad] floats.
+  __shared__ __attribute__((aligned(1024))) char ring[kWaves * 2 * kHalf];
+  static_assert(kWaves * 16 * kPad * 4 <= (int)sizeof(ring), "the results of a tile of rows fit");
+  float (*const red)[16][kPad] = reinterpret_cast<float (*)[16][kPad]>(ring);
   __shared__ float red_m[kWaves][kRows], red_l[kWaves][kRows];
   __shared__ int64_t wave_tiles[kWaves];
   __shared__ int64_t found[2];
@@ -77,9 +129,9 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
   const CacheArgs& c = a.cache;
 
   // ---- this workgroup's range of tiles ----
-  const int per = (c.n_seqs + 255) / 256, s_first = min(tid * per, c.n_seqs), s_last = min(s_first + per, c.n_seqs);
+  const int per = (c.n_seqs + kThreads - 1) / kThreads, s_first = min(tid * per, c.n_seqs), s_last = min(s_first + per, c.n_seqs);
   auto tiles_of_seq = [&](int s) {
-    const PairShape p = pairs_of<kRows>(a, rows_of_seq(c, s));
+    const PairShape p = pairs_of<kRows>(a, rows_of_seq(c, s), tile);
     return (int64_t)p.groups * a.Hkv * p.tiles;
   };
   int64_t mine = 0;
@@ -104,10 +156,10 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
     for (int s = s_first; s < s_last; ++s) { part.prefix[s] = x; x += tiles_of_seq(s); }
     if (tid == 0) part.prefix[c.n_seqs] = total;
   }
-  const int n = (int)min((int64_t)n_groups, total);     // ranges, none of them empty
-  if ((int)blockIdx.x >= n) return;
-  int64_t t = range_begin(total, blockIdx.x, n);
-  const int64_t t_end = range_begin(total, blockIdx.x + 1, n);
+  const int64_t each = uniform64(tiles_each(total, n_groups));
+  int64_t t = blockIdx.x * each;
+  const int64_t t_end = min(t + each, total);
+  if (t >= t_end) return;
   if (upto - mine <= t && t < upto) {                   // one thread
     int64_t x = upto - mine;
     int s = s_first;
@@ -124,15 +176,22 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
   int64_t base = uniform64(found[1]);
 
   const float sc = a.scale * kLog2e;
-  while (t < t_end) {
-    const SeqRows r = rows_of_seq(c, seq);
-    const PairShape shape = pairs_of<kRows>(a, r);
-    const int64_t n_seq = (int64_t)shape.groups * a.Hkv * shape.tiles;
+  for (;;) {
+    t = uniform64(t);
+    base = uniform64(base);
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    if (t >= t_end) break;
+    SeqRows r = rows_of_seq(c, seq);
+    r.first = __builtin_amdgcn_readfirstlane(r.first);
+    r.count = __builtin_amdgcn_readfirstlane(r.count);
+    r.length = __builtin_amdgcn_readfirstlane(r.length);
+    const PairShape shape = pairs_of<kRows>(a, r, tile);
+    const int64_t n_seq = uniform64((int64_t)shape.groups * a.Hkv * shape.tiles);
     if (t >= base + n_seq) { base += n_seq; ++seq; continue; }
-    const int64_t pair = (t - base) / shape.tiles;
-    const int tile0 = (int)(t - base - pair * shape.tiles);
-    const int tile1 = (int)min((int64_t)shape.tiles, tile0 + (t_end - t));
-    const int kvh = __builtin_amdgcn_readfirstlane((int)(pair / shape.groups)), group0 = (int)(pair - (int64_t)kvh * shape.groups) * kRows;
+    const int64_t pair = uniform64(quotient(t - base, shape.tiles));
+    const int tile0 = __builtin_amdgcn_readfirstlane((int)(t - base - pair * shape.tiles));
+    const int tile1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)shape.tiles, tile0 + (t_end - t)));
+    const int kvh = __builtin_amdgcn_readfirstlane((int)quotient(pair, shape.groups)), group0 = __builtin_amdgcn_readfirstlane((int)(pair - (int64_t)kvh * shape.groups) * kRows);
     t += tile1 - tile0;
 
     // ---- rows ----
@@ -150,7 +209,7 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
     }
     const int hi_max = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)(min(group0 + kRows, n_list) - 1) / a.group_div));
     const int hi_min = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)group0 / a.group_div));
-    const int key_end = min(tile1 * kTile, hi_max + 1);
+    const int key_end = __builtin_amdgcn_readfirstlane(min((int)min((int64_t)tile1 * (int)tile.d, (int64_t)INT32_MAX), hi_max + 1));
 
     bool odd = false;                                   // this lane has left out an infinity or NaN of V
     f32x4 acc[kNT][kAcc];
@@ -165,8 +224,18 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
 
     const char* const k_head = c.k + kvh * c.head_stride * kElt;
     const char* const v_head = c.v + kvh * c.head_stride * kElt;
-    const uint32_t k_lane = (uint32_t)(col * c.tok_stride * kElt + quad * 16), v_lane = (uint32_t)(quad * 4 * c.tok_stride * kElt + col * 16);
-    const uint32_t v_step = (uint32_t)(c.tok_stride * kElt);
+    // Copy t of a block takes 64 / kRowChunks of its keys, 1 KiB: lane -> (key, 16-byte place).  A row of K has its pieces in places place ^ key, so that 16 lanes that read the
+    // same piece of 16 keys find them in different banks.  V is read a row at a time, by 16 lanes.
+    constexpr int kRowChunks = kD * kElt / 16, kBlockCopies = kCopies / kBlocks;
+    const uint32_t row_bytes = (uint32_t)c.tok_stride * kElt, key_lane = (uint32_t)lane / kRowChunks, place = (uint32_t)lane % kRowChunks;
+    uint32_t k_lane[kBlockCopies];
+#pragma unroll
+    for (int i = 0; i < kBlockCopies; ++i) {
+      const uint32_t key = i * (64 / kRowChunks) + key_lane;
+      k_lane[i] = key * row_bytes + (place ^ (key & 15)) * 16;
+    }
+    const uint32_t v_lane = key_lane * row_bytes + place * 16;
+    const char* const k_ring = ring + wave * 2 * kHalf, * const v_ring = k_ring + kHalf;
     const int32_t* const table = c.table + seq * c.table_stride;
 
     // Steps of this wavefront, kKeys keys each: step i takes keys key_of(i) .. + kKeys.  A refill looks up the pages of the next 64
@@ -176,24 +245,19 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
       uint32_t here;                                    // bit b: block b lies in this pool
       int64_t at[kBlocks];                              // where the blocks lie, in bytes
     };
-    auto key_of = [&](int i) { return tile0 * kTile + (i * kWaves + wave) * kKeys; };
-    int ahead = 0, pages = 0, end = 0;                  // first step of the refill; page of this lane's block; keys end here
+    auto key_of = [&](int i) { return tile0 * (int)tile.d + (i * kWaves + wave) * kKeys; };
+    int ahead = 0, pages = 0;                           // first step of the refill; page of this lane's block
     uint64_t todo = 0;                                  // blocks of the refill that are here and not fetched
     auto refill = [&] {
       const int kb = key_of(ahead + lane / kBlocks) + 16 * (lane % kBlocks);
-      pages = kb < end ? table[(uint32_t)kb / c.page_div] : -1;
-      todo = __ballot(pages >= 0 && pages < c.n_pages);
-    };
-    auto begin = [&](int first, int to) {
-      ahead = first;
-      end = to;
-      todo = 0;
-      if (key_of(first) < to) refill();
+      // without a branch by lane: a loop that has none keeps its addresses in scalar registers
+      pages = table[(uint32_t)min(kb, key_end - 1) / c.page_div];
+      todo = __ballot(kb < key_end && pages >= 0 && pages < c.n_pages);
     };
     auto next = [&](Step& x) {
       while (todo == 0) {
         ahead += 64 / kBlocks;
-        if (key_of(ahead) >= end) return false;
+        if (key_of(ahead) >= key_end) return false;
         refill();
       }
       const int i = __builtin_ctzll(todo) / kBlocks;
@@ -208,25 +272,34 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
       }
       return true;
     };
-    // Read once, past the caches: 7.1 TB/s in a large plain read where the default policy reaches 6.2.
-    u32x4 k[kBlocks][kKL], v[kBlocks][4][kVC];
-    auto load_k = [&](const Step& x) {
+    auto copy_k = [&](const Step& x) {
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int e = 0; e < kKL; ++e) k[b][e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k_head + x.at[b] + k_lane + e * 64));
+        for (int i = 0; i < kBlockCopies; ++i) copy_past_caches(k_head + x.at[b], k_lane[i], ring, wave * 2 * kHalf + (b * kBlockCopies + i) * 1024);
     };
-    auto load_v = [&](const Step& x) {
+    auto copy_v = [&](const Step& x) {
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int e = 0; e < kVC; ++e) v[b][r][e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v_head + x.at[b] + v_lane + r * v_step + e * 256));
+        for (int i = 0; i < kBlockCopies; ++i)
+          copy_past_caches(v_head + x.at[b] + (int64_t)i * (64 / kRowChunks) * row_bytes, v_lane, ring, wave * 2 * kHalf + kHalf + (b * kBlockCopies + i) * 1024);
     };
-    // edge: the step has keys that some rows see and others do not.  Computes a step, and asks for the following one's K and V as soon as the registers that they go to are free.
+    // edge: the step has keys that some rows see and others do not.  The step's copies are on their way, K's before V's; the following step's K is asked for as soon as this
+    // one's has been read, and so is V.
     auto compute = [&](const Step& x, auto edge, auto has_next, const Step& after) {
       const bool whole = !decltype(edge)::value && x.k0 + kKeys - 1 <= hi_max && x.here == (1u << kBlocks) - 1;   // every row sees every key
+
+      wait_copies<kCopies>();                            // V's may be under way
+      u32x4 k[kBlocks][kKL];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < kKL; ++i) k[b][i] = *reinterpret_cast<const u32x4*>(k_ring + (b * 16 + col) * kD * kElt + ((i * 4 + quad) ^ col) * 16);
+      if constexpr (decltype(has_next)::value) {
+        wait_reads();
+        copy_k(after);
+      }
 
       // P^T: lane (col, quad) holds row col, keys 16 b + 4 quad + i
       f32x4 p[kNT][kBlocks];
@@ -251,7 +324,6 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
           p[j][b] = s;
         }
       }
-      if constexpr (decltype(has_next)::value) load_k(after);
 #pragma unroll
       for (int j = 0; j < kNT; ++j) {
         float top = p[j][0][0];
@@ -307,6 +379,18 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
         seen[y] = bits(in && key <= hi_max, in && key + 1 <= hi_max);
         some[y] = bits(key > hi_min, key + 1 > hi_min);
       }
+      wait_copies<decltype(has_next)::value ? kCopies : 0>();   // K's of the next step may be under way
+      u32x4 v[kBlocks][4][kVC];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int e = 0; e < kVC; ++e) v[b][r][e] = *reinterpret_cast<const u32x4*>(v_ring + (b * 16 + quad * 4 + r) * kD * kElt + (e * 16 + col) * 16);
+      if constexpr (decltype(has_next)::value) {
+        wait_reads();
+        copy_v(after);
+      }
       auto add_pv = [&](auto some_too) {
         auto word = [&](uint32_t w, int y) {
           w &= seen[y];
@@ -344,31 +428,37 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
         }
       };
       add_pv(edge);
-      if constexpr (decltype(has_next)::value) load_v(after);
     };
-    // keys [0, edge) are seen by all rows or, from hi_max + 1 on, by none
-    const int edge = hi_min == hi_max ? key_end : min(key_end, max(0, hi_min + 1) / kKeys * kKeys);
+    // Wait for Q here, once: left to the compiler the wait would stand in the loop, where the same counter holds the copies.
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int i = 0; i < kKL; ++i) asm volatile("" : "+v"(q[j][i]));
+    auto on_edge = [&](const Step& x) { return hi_min < hi_max && x.k0 + kKeys - 1 > hi_min; };   // the last steps, where rows differ in what they see
     Step now, after;
-    begin(0, edge);
-    if (next(now)) {
-      load_k(now);
-      load_v(now);
-      while (next(after)) {
-        compute(now, std::false_type(), std::true_type(), after);
-        now = after;
-      }
-      compute(now, std::false_type(), std::false_type(), now);
+    if (key_of(0) < key_end) refill();
+    bool have = next(now);
+    if (have) {
+      copy_k(now);
+      copy_v(now);
     }
-    if (edge < key_end) {
-      begin(max(0, edge - tile0 * kTile + (kWaves - 1 - wave) * kKeys) / (kWaves * kKeys), key_end);   // the first step with keys from `edge` on
-      while (next(now)) {
-        load_k(now);
-        load_v(now);
-        compute(now, std::true_type(), std::false_type(), now);
+    while (have && !on_edge(now)) {
+      have = next(after);
+      if (have) compute(now, std::false_type(), std::true_type(), after);
+      else compute(now, std::false_type(), std::false_type(), now);
+      now = after;
+    }
+    while (have) {
+      compute(now, std::true_type(), std::false_type(), now);
+      have = next(now);
+      if (have) {
+        wait_reads();
+        copy_k(now);
+        copy_v(now);
       }
     }
     if (__any(odd)) {
-      for (int key = max(tile0 * kTile, hi_min + 1); key < key_end; ++key) {
+      for (int key = max(tile0 * (int)tile.d, hi_min + 1); key < key_end; ++key) {
         const int tp = (int)((uint32_t)key / c.page_div), page = table[tp];
         if (page < 0 || page >= c.n_pages) continue;
         const char* const row = v_head + (page * c.page_stride + (key - tp * c.page_size) * c.tok_stride) * kElt;
@@ -396,6 +486,7 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
         red_l[wave][j * 16 + col] = l[j];
       }
     }
+    __syncthreads();                                    // every wavefront has read its last K and V
     const bool finished = tile0 == 0 && tile1 == shape.tiles;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (tile0 == 0 ? 1 : 0);
 #pragma unroll
@@ -409,8 +500,8 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
           *reinterpret_cast<f32x4*>(&red[wave][col][d]) = f32x4{acc[j][e][i], acc[j][e + 1][i], acc[j][e + 2][i], acc[j][e + 3][i]};
         }
       __syncthreads();
-      const int row = tid >> 4, jr = j * 16 + row;       // 16 threads share a row
-      constexpr int kEach = kD / 16;
+      constexpr int kShare = kThreads / 16, kEach = kD / kShare;   // threads of a row, elements of each
+      const int row = tid / kShare, jr = j * 16 + row, d0 = tid % kShare * kEach;
       float top = red_m[0][jr];
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w][jr]);
@@ -423,33 +514,22 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
         const float f = __builtin_amdgcn_exp2f(red_m[w][jr] - ref);
         sum += f * red_l[w][jr];
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) x[e] += f * red[w][row][(tid & 15) * kEach + e];
+        for (int e = 0; e < kEach; ++e) x[e] += f * red[w][row][d0 + e];
       }
       const int i = group0 + jr;
       if (i < n_list) {
         if (finished) {
           const int tok = (int)((uint32_t)i / a.group_div), h = kvh * a.group + i - tok * a.group;
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          const int64_t at = ((int64_t)(r.first + tok) * a.Hq + h) * kD + (tid & 15) * kEach;
+          const int64_t at = ((int64_t)(r.first + tok) * a.Hq + h) * kD + d0;
 #pragma unroll
           for (int e = 0; e < kEach; ++e) x[e] *= inv;
-          if (a.o != nullptr)
-#pragma unroll
-            for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(a.o + at + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-          if (a.o_final != nullptr) {
-            if constexpr (kBf16) {
-              *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.o_final) + at) = mk4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
-            } else {
-#pragma unroll
-              for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.o_final) + at + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-            }
-          }
-          if (a.lse != nullptr && (tid & 15) == 0) a.lse[h * a.lse_hs + r.first + tok] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+          if (a.o != nullptr) store_row<false>(a.o, at, x);
+          if (a.o_final != nullptr) store_row<kBf16>(a.o_final, at, x);
+          if (a.lse != nullptr && d0 == 0) a.lse[h * a.lse_hs + r.first + tok] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
         } else {
-          float* const to = part.o + (slot * kRows + jr) * kD + (tid & 15) * kEach;
-#pragma unroll
-          for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-          if ((tid & 15) == 0) { part.m[slot * kRows + jr] = top; part.l[slot * kRows + jr] = sum; }
+          store_row<false>(part.o, (slot * kRows + jr) * kD + d0, x);
+          if (d0 == 0) { part.m[slot * kRows + jr] = top; part.l[slot * kRows + jr] = sum; }
         }
       }
       __syncthreads();
@@ -457,72 +537,114 @@ __global__ __launch_bounds__(256, kNT == 1 ? 2 : 1) void cache_attn_kernel(Cache
   }
 }
 
-// Joins the partial results of pairs that several workgroups shared.  A workgroup takes one (row, head); teams of d / 4 threads share out the partial results.
+// Joins the partial results of pairs that several workgroups shared.  A workgroup takes one (row, head); teams of d / 4 threads share out the partial
+// results.  It is a chain of latencies: which sequence and which partial results, these with their maxima and sums, the result.  All that one
+// of them needs is asked for at once: 28 workgroups that join 128 partial results each took 10.8 us with maxima, sums and results after one another, and take XX.
 template <bool kBf16, int kD, int kRows>
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a, int n_groups, Partial part) {
-  constexpr int kTeam = kD / 4, kTeams = 256 / kTeam;
+__global__ __launch_bounds__(256, JO) void cache_join_kernel(CacheAttnArgs a, int n_groups, FastDiv tile, Partial part) {
+  constexpr int kTeam = kD / 4, kTeams = 256 / kTeam, kBatch = JB;
   __shared__ f32x4 xs[kTeams][kTeam];
-  __shared__ float ms[kTeams], ls[kTeams];
+  __shared__ float ls[kTeams], tops[4], ms[kMaxGroups], sums[kMaxGroups];
+  __shared__ int before[4];
   const CacheArgs& c = a.cache;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.x / a.Hq, h = blockIdx.x - row * a.Hq;
-  const int seq = seq_of_row(c, row);
-  if (seq < 0) return;
+  int seq = row;
+  if (c.cu_new != nullptr && c.n_seqs <= 1024) {        // counted, not searched for: one latency
+    int n = 0;
+    for (int s = tid; s < c.n_seqs; s += 256) n += c.cu_new[s + 1] <= row;
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) n += __shfl_xor(n, w);
+    if (lane == 0) before[wave] = n;
+    __syncthreads();
+    seq = before[0] + before[1] + before[2] + before[3];
+  } else if (c.cu_new != nullptr) {
+    seq = seq_of_row(c, row);
+  }
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  if (seq < 0 || seq >= c.n_seqs) return;
   const SeqRows r = rows_of_seq(c, seq);
-  const PairShape shape = pairs_of<kRows>(a, r);
-  const int kvh = (int)((uint32_t)h / a.group_div), i = (row - r.first) * a.group + h - kvh * a.group;
-  if (i < 0 || row - r.first >= r.count) return;
+  if (row < r.first || row - r.first >= r.count) return;
+  const PairShape shape = pairs_of<kRows>(a, r, tile);
+  const int kvh = (int)((uint32_t)h / a.group_div), i = (row - r.first) * a.group + h - kvh * a.group, jr = i % kRows;
   const int64_t total = part.prefix[c.n_seqs], t0 = part.prefix[seq] + ((int64_t)kvh * shape.groups + i / kRows) * shape.tiles;
-  const int n = (int)min((int64_t)n_groups, total);
-  const int w0 = range_of(total, t0, n), w1 = range_of(total, t0 + shape.tiles - 1, n), count = w1 - w0 + 1;
+  const int64_t each = tiles_each(total, n_groups);
+  const int w0 = (int)quotient(t0, each), count = (int)quotient(t0 + shape.tiles - 1, each) - w0 + 1;
   if (count == 1) return;                               // finished where it was computed
-  const int team = threadIdx.x / kTeam, e = threadIdx.x % kTeam, jr = i % kRows;
-  auto slot = [&](int s) { return 2 * (int64_t)(w0 + s) + (s == 0 ? 1 : 0); };
+  const int team = tid / kTeam, e = tid % kTeam;
+  auto at = [&](int s) { return (2 * (int64_t)(w0 + s) + (s == 0 ? 1 : 0)) * kRows + jr; };
+  f32x4 y[kBatch];
+  auto ask = [&](int first) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int s = first + k * kTeams + team;
+      y[k] = s < count ? *reinterpret_cast<const f32x4*>(part.o + at(s) * kD + e * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  ask(0);
   float top = -INFINITY;
-  for (int s = team; s < count; s += kTeams) top = fmaxf(top, part.m[slot(s) * kRows + jr]);
-  float ref = top == -INFINITY ? 0.f : top, sum = 0.f;
+  for (int s = tid; s < count; s += 256) {
+    const float m = part.m[at(s)];
+    ms[s] = m;
+    sums[s] = part.l[at(s)];
+    top = fmaxf(top, m);
+  }
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int s = team; s < count; s += kTeams) {
-    const int64_t at = slot(s) * kRows + jr;
-    const float f = __builtin_amdgcn_exp2f(part.m[at] - ref);
-    sum += f * part.l[at];
-    x += f * *reinterpret_cast<const f32x4*>(part.o + at * kD + e * 4);
+  for (int first = 0; first < count; first += kBatch * kTeams) {
+    if (first > 0) ask(first);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int s = min(first + k * kTeams + team, count - 1);
+      const bool live = first + k * kTeams + team < count;
+      const float f = __builtin_amdgcn_exp2f(ms[s] - ref);
+      sum += live ? f * sums[s] : 0.f;
+      x += live ? f * y[k] : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
   }
   xs[team][e] = x;
-  if (e == 0) { ms[team] = top; ls[team] = sum; }
+  if (e == 0) ls[team] = sum;
   __syncthreads();
   if (team != 0) return;
-  for (int k = 0; k < kTeams; ++k) top = fmaxf(top, ms[k]);
-  ref = top == -INFINITY ? 0.f : top;
   sum = 0.f;
   x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
   for (int k = 0; k < kTeams; ++k) {
-    const float f = __builtin_amdgcn_exp2f(ms[k] - ref);
-    sum += f * ls[k];
-    x += f * xs[k][e];
+    sum += ls[k];
+    x += xs[k][e];
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   x *= inv;
-  const int64_t at = ((int64_t)row * a.Hq + h) * kD + e * 4;
-  if (a.o != nullptr) *reinterpret_cast<f32x4*>(a.o + at) = x;
+  const int64_t to = ((int64_t)row * a.Hq + h) * kD + e * 4;
+  if (a.o != nullptr) *reinterpret_cast<f32x4*>(a.o + to) = x;
   if (a.o_final != nullptr) {
-    if constexpr (kBf16) *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.o_final) + at) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
-    else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.o_final) + at) = x;
+    if constexpr (kBf16) *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.o_final) + to) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.o_final) + to) = x;
   }
   if (a.lse != nullptr && e == 0) a.lse[h * a.lse_hs + row] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// How a call is laid out: tiles of 16 rows of a workgroup's group, workgroups.
-struct Plan { int nt, groups; };
+// How a call is laid out: tiles of 16 rows of a workgroup's group, workgroups, keys of a tile, and whether several workgroups may share a pair.
+struct Plan { int nt, groups, tile; bool shared; };
 Plan plan_of(const CacheAttnArgs& a) {
   const CacheArgs& c = a.cache;
-  // As many rows as a sequence has on average in one group, up to 64: every further group reads the keys again.
+  // As many rows as a sequence has on average in one group, up to 48: every further group reads the keys again.
   const int64_t mean = ((int64_t)c.n_rows * a.group + c.n_seqs - 1) / c.n_seqs;
   Plan p;
-  p.nt = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
-  const int64_t rows = 16 * p.nt, capacity = (int64_t)c.max_pages * c.page_size;
-  const int64_t pairs = ((int64_t)c.n_rows * a.group / rows + c.n_seqs) * a.Hkv, room = (int64_t)cu_count() * (p.nt == 1 ? 2 : 1);
-  p.groups = (int)std::min(room, std::min(pairs, room) * std::max<int64_t>(1, (capacity + kTile - 1) / kTile));
+  p.nt = mean <= 16 ? 1 : mean <= 32 ? 2 : 3;
+  const int round = kRound * (p.nt == 1 ? waves_of<1>() : waves_of<2>());
+  const int64_t rows = 16 * p.nt, capacity = (int64_t)c.max_pages * c.page_size, rounds = std::max<int64_t>(1, (capacity + round - 1) / round);
+  // A cache of a few rounds: one workgroup for a pair, and no second launch.
+  p.shared = rounds > kWholeRounds;
+  p.tile = p.shared ? round : (int)rounds * round;
+  const int64_t pairs = ((int64_t)c.n_rows * a.group / rows + c.n_seqs) * a.Hkv, room = std::min(kMaxGroups, cu_count());
+  p.groups = (int)std::min(room, std::min(pairs, room) * (p.shared ? rounds : 1));
   return p;
 }
 
@@ -550,17 +672,17 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t s
   auto launch = [&](auto bf16, auto d, auto nt) {
     constexpr bool kBf16 = decltype(bf16)::value;
     constexpr int kD = decltype(d)::value, kNT = decltype(nt)::value;
-    cache_attn_kernel<kBf16, kD, kNT><<<dim3((unsigned)p.groups), dim3(256), 0, stream>>>(a, p.groups, part);
+    cache_attn_kernel<kBf16, kD, kNT><<<dim3((unsigned)p.groups), dim3(64 * waves_of<kNT>()), 0, stream>>>(a, p.groups, fast_div(p.tile), part);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.groups == 1) return e;
-    cache_join_kernel<kBf16, kD, 16 * kNT><<<dim3((unsigned)((int64_t)a.cache.n_rows * a.Hq)), dim3(256), 0, stream>>>(a, p.groups, part);
+    if (e != hipSuccess || !p.shared || p.groups == 1) return e;
+    cache_join_kernel<kBf16, kD, 16 * kNT><<<dim3((unsigned)((int64_t)a.cache.n_rows * a.Hq)), dim3(256), 0, stream>>>(a, p.groups, fast_div(p.tile), part);
     return hipGetLastError();
   };
   auto by_rows = [&](auto bf16, auto d) {
     switch (p.nt) {
       case 1: return launch(bf16, d, std::integral_constant<int, 1>());
       case 2: return launch(bf16, d, std::integral_constant<int, 2>());
-      default: return launch(bf16, d, std::integral_constant<int, 4>());
+      default: return launch(bf16, d, std::integral_constant<int, 3>());
     }
   };
   if (io_dtype == 0) return by_rows(std::true_type(), std::integral_constant<int, 128>());
