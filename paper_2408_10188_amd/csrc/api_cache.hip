@@ -214,6 +214,9 @@ mmsp_status mmsp_cache_attn(const mmsp_shape* shape, const mmsp_cache* cache, co
     return fail(MMSP_ERR_UNSUPPORTED, "%d rows x %d heads: more than 2^23 are not supported", cache->n_rows, shape->n_q_heads);
   if (cache->n_rows == 0 || cache->n_seqs == 0) return MMSP_OK;
   CacheAttnArgs a = attn_args(shape, cache);
+  if (cache_attn_tiles(a, shape->io_dtype) >= 0x1p31)
+    return fail(MMSP_ERR_UNSUPPORTED, "%d sequences of up to %d pages of %d tokens and %d KV heads are too much for a call", cache->n_seqs, cache->max_pages,
+                cache->page_size, shape->n_kv_heads);
   const size_t need = (size_t)cache_attn_workspace_bytes(a, shape->io_dtype);
   if (workspace == nullptr || workspace_bytes < need)
     return fail(MMSP_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes given, %zu needed (mmsp_cache_workspace_bytes)", workspace_bytes, need);

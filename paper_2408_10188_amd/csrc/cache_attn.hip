@@ -23,23 +23,24 @@ namespace {
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
-#ifndef WR
-#define WR 4
-#endif
-constexpr int kWholeRounds = WR;
 #ifndef JB
 #define JB 4
 #endif
 #ifndef JO
 #define JO 8
 #endif
-// Wavefronts of a workgroup: two on each SIMD, or one with all of its registers where there are more than 16 rows.
-template <int kNT> constexpr int waves_of() { return kNT == 1 ? 8 : 4; }
-constexpr int kRound = 32;                              // keys of a tile: a multiple of this times the wavefronts
+#ifndef WR
+#define WR 4
+#endif
+#ifndef MS
+#define MS 8
+#endif
+constexpr int kWholeSteps = WR;
+constexpr int kMostSplit = MS;
 constexpr int kMaxGroups = 1024;                        // workgroups of a launch
 
 struct Partial {
-  int64_t* prefix;                                      // [n_seqs + 1] tiles of the sequences before
+  int32_t* prefix;                                      // [n_seqs + 1] tiles of the sequences before, then the logarithm of a tile's keys
   float* m; float* l;                                   // [2 W][kRows]
   float* o;                                             // [2 W][kRows][d]
 };
@@ -47,10 +48,10 @@ struct Partial {
 // Groups of kRows rows of a KV head's list, and tiles of each of their pairs.
 struct PairShape { int groups, tiles; };
 template <int kRows>
-__device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const SeqRows& r, const FastDiv& tile) {
+__device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const SeqRows& r, int tile_bits) {
   PairShape p;
   p.groups = (int)(((int64_t)r.count * a.group + kRows - 1) / kRows);
-  p.tiles = max(1, (int)((uint32_t)(r.length + (int)tile.d - 1) / tile));   // rows that see nothing have a tile too: someone has to say so
+  p.tiles = max(1, (r.length + (1 << tile_bits) - 1) >> tile_bits);   // rows that see nothing have a tile too: someone has to say so
   return p;
 }
 
@@ -98,17 +99,30 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
   else return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
 }
 
-// The quotient of numbers that almost always fit 32 bits; a 64-bit division is over a hundred dependent instructions.
-__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
-  if ((uint64_t)(x | y) >> 32 == 0) return (uint32_t)x / (uint32_t)y;
-  return x / y;
-}
-// Tiles of a workgroup's range: workgroup w has tiles [w * each, (w + 1) * each) of `total`.
-__device__ __forceinline__ int64_t tiles_each(int64_t total, int n_groups) { return quotient(total + n_groups - 1, n_groups); }
+// Tiles of a workgroup's range: workgroup w has tiles [w * each, (w + 1) * each) of `total`.  (The host has made sure that there are fewer than 2^31.)
+__device__ __forceinline__ int tiles_each(int total, int n_groups) { return max(1, (int)(((uint32_t)total + n_groups - 1) / (uint32_t)n_groups)); }
 
-template <bool kBf16, int kD, int kNT>
-__global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a, int n_groups, FastDiv tile, Partial part) {
-  constexpr int kWaves = waves_of<kNT>(), kThreads = 64 * kWaves;
+// Keys of a tile, as a logarithm: the fewest, from a step of four wavefronts on, with which every workgroup has at most one tile, or else kMostSplit, the one with the least waste where workgroups
+// go through several segments.  tiles(bits): those of this lane's sequence.
+template <int kFewest, class Tiles>
+__device__ __forceinline__ int pick_tile(Tiles tiles, int n_groups) {
+  constexpr int kMost = 9;
+  int n[kMost - kFewest + 1];
+#pragma unroll
+  for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] = min(tiles(b), 1 << 24);   // 64 of them stay below 2^31
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1)
+#pragma unroll
+    for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] += __shfl_xor(n[b - kFewest], w);
+  int bits = kMostSplit;
+#pragma unroll
+  for (int b = kMost; b >= kFewest; --b) bits = n[b - kFewest] <= n_groups ? b : bits;
+  return __builtin_amdgcn_readfirstlane(bits);
+}
+
+template <bool kBf16, int kD, int kNT, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kNT <= 2 ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a, int n_groups, int tile_bits, Partial part) {
+  constexpr int kThreads = 64 * kWaves;
   constexpr int kRows = 16 * kNT, kElt = kBf16 ? 2 : 4;
   constexpr int kBlocks = kBf16 ? 2 : 1, kKeys = 16 * kBlocks;   // blocks of 16 keys, keys of a step
   constexpr int kKL = kD * kElt / 64;                   // 16-byte pieces of a K row that a lane holds
@@ -121,77 +135,112 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
   static_assert(kWaves * 16 * kPad * 4 <= (int)sizeof(ring), "the results of a tile of rows fit");
   float (*const red)[16][kPad] = reinterpret_cast<float (*)[16][kPad]>(ring);
   __shared__ float red_m[kWaves][kRows], red_l[kWaves][kRows];
-  __shared__ int64_t wave_tiles[kWaves];
-  __shared__ int64_t found[2];
+  __shared__ int wave_tiles[kWaves], found[2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quad = lane >> 4;
   const CacheArgs& c = a.cache;
 
   // ---- this workgroup's range of tiles ----
-  const int per = (c.n_seqs + kThreads - 1) / kThreads, s_first = min(tid * per, c.n_seqs), s_last = min(s_first + per, c.n_seqs);
-  auto tiles_of_seq = [&](int s) {
-    const PairShape p = pairs_of<kRows>(a, rows_of_seq(c, s), tile);
-    return (int64_t)p.groups * a.Hkv * p.tiles;
+  // (Every bound below also holds where cu_new is not ascending and the sums are nonsense.)
+  auto tiles_of = [&](const SeqRows& r, int bits) {
+    const PairShape p = pairs_of<kRows>(a, r, bits);
+    return p.groups * a.Hkv * p.tiles;
   };
-  int64_t mine = 0;
-  for (int s = s_first; s < s_last; ++s) mine += tiles_of_seq(s);
-  int64_t upto = mine;                                  // of the threads up to this one
+  const bool few = c.n_seqs <= 64;                      // every wavefront has all sequences in its lanes: no LDS, no second look at memory
+  SeqRows mine = {};                                    // of sequence `lane`, if few
+  int t, t_end, seq, base;                              // the next tile, the range's end; the tile's sequence, and tiles before that one
+  if (few) {
+    if (lane < c.n_seqs) mine = rows_of_seq(c, lane);
+    if (tile_bits < 0) tile_bits = pick_tile<kBf16 ? 7 : 6>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, n_groups);
+    const int n = lane < c.n_seqs ? tiles_of(mine, tile_bits) : 0;
+    int upto = n;
 #pragma unroll
-  for (int w = 1; w < 64; w <<= 1) {
-    const int64_t x = __shfl_up(upto, w);
-    if (lane >= w) upto += x;
-  }
-  if (lane == 63) wave_tiles[wave] = upto;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) upto += wave_tiles[w];
-    total += wave_tiles[w];
-  }
-  total = uniform64(total);
-  if (blockIdx.x == 0) {                                // for the joining launch
-    int64_t x = upto - mine;
-    for (int s = s_first; s < s_last; ++s) { part.prefix[s] = x; x += tiles_of_seq(s); }
-    if (tid == 0) part.prefix[c.n_seqs] = total;
-  }
-  const int64_t each = uniform64(tiles_each(total, n_groups));
-  int64_t t = blockIdx.x * each;
-  const int64_t t_end = min(t + each, total);
-  if (t >= t_end) return;
-  if (upto - mine <= t && t < upto) {                   // one thread
-    int64_t x = upto - mine;
-    int s = s_first;
-    for (;; ++s) {
-      const int64_t y = tiles_of_seq(s);
-      if (t < x + y) break;
-      x += y;
+    for (int w = 1; w < 64; w <<= 1) {
+      const int x = __shfl_up(upto, w);
+      if (lane >= w) upto += x;
     }
-    found[0] = s;
-    found[1] = x;
+    const int total = __builtin_amdgcn_readlane(upto, 63);
+    if (blockIdx.x == 0 && wave == 0) {                 // for the joining launch
+      if (lane < c.n_seqs) part.prefix[lane] = upto - n;
+      if (lane == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
+    }
+    const int each = tiles_each(total, n_groups);
+    t = blockIdx.x * each;
+    t_end = min(t + each, total);
+    if (t >= t_end) return;
+    seq = 63 - __builtin_clzll(__ballot(lane < c.n_seqs && upto - n <= t) | 1);   // the last one that begins by then
+    base = __builtin_amdgcn_readlane(upto - n, seq);
+  } else {
+    if (tile_bits < 0) tile_bits = kMostSplit;
+    const int per = (c.n_seqs + kThreads - 1) / kThreads, s_first = min(tid * per, c.n_seqs), s_last = min(s_first + per, c.n_seqs);
+    int n = 0;
+    for (int s = s_first; s < s_last; ++s) n += tiles_of(rows_of_seq(c, s), tile_bits);
+    int upto = n;                                       // of the threads up to this one
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) {
+      const int x = __shfl_up(upto, w);
+      if (lane >= w) upto += x;
+    }
+    if (lane == 63) wave_tiles[wave] = upto;
+    if (tid == 0) found[0] = c.n_seqs;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) upto += wave_tiles[w];
+      total += wave_tiles[w];
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    if (blockIdx.x == 0) {
+      int x = upto - n;
+      for (int s = s_first; s < s_last; ++s) { part.prefix[s] = x; x += tiles_of(rows_of_seq(c, s), tile_bits); }
+      if (tid == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
+    }
+    const int each = tiles_each(total, n_groups);
+    t = blockIdx.x * each;
+    t_end = min(t + each, total);
+    if (t >= t_end) return;
+    if (upto - n <= t && t < upto) {                    // one thread
+      int x = upto - n, s = s_first;
+      for (; s < s_last; ++s) {
+        const int y = tiles_of(rows_of_seq(c, s), tile_bits);
+        if (t < x + y) break;
+        x += y;
+      }
+      found[0] = s;
+      found[1] = x;
+    }
+    __syncthreads();
+    seq = found[0];
+    base = found[1];
   }
-  __syncthreads();
-  int seq = __builtin_amdgcn_readfirstlane((int)found[0]);
-  int64_t base = uniform64(found[1]);
 
   const float sc = a.scale * kLog2e;
   for (;;) {
-    t = uniform64(t);
-    base = uniform64(base);
+    // scalars, whatever the compiler makes of the above: the addresses of K and V hang on them
+    t = __builtin_amdgcn_readfirstlane(t);
+    base = __builtin_amdgcn_readfirstlane(base);
     seq = __builtin_amdgcn_readfirstlane(seq);
-    if (t >= t_end) break;
-    SeqRows r = rows_of_seq(c, seq);
-    r.first = __builtin_amdgcn_readfirstlane(r.first);
-    r.count = __builtin_amdgcn_readfirstlane(r.count);
-    r.length = __builtin_amdgcn_readfirstlane(r.length);
-    const PairShape shape = pairs_of<kRows>(a, r, tile);
-    const int64_t n_seq = uniform64((int64_t)shape.groups * a.Hkv * shape.tiles);
+    if (t >= t_end || seq >= c.n_seqs) break;
+    SeqRows r;
+    if (few) {
+      r.first = __builtin_amdgcn_readlane(mine.first, seq);
+      r.count = __builtin_amdgcn_readlane(mine.count, seq);
+      r.length = __builtin_amdgcn_readlane(mine.length, seq);
+    } else {
+      r = rows_of_seq(c, seq);
+      r.first = __builtin_amdgcn_readfirstlane(r.first);
+      r.count = __builtin_amdgcn_readfirstlane(r.count);
+      r.length = __builtin_amdgcn_readfirstlane(r.length);
+    }
+    const PairShape shape = pairs_of<kRows>(a, r, tile_bits);
+    const int n_seq = shape.groups * a.Hkv * shape.tiles;
     if (t >= base + n_seq) { base += n_seq; ++seq; continue; }
-    const int64_t pair = uniform64(quotient(t - base, shape.tiles));
-    const int tile0 = __builtin_amdgcn_readfirstlane((int)(t - base - pair * shape.tiles));
-    const int tile1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)shape.tiles, tile0 + (t_end - t)));
-    const int kvh = __builtin_amdgcn_readfirstlane((int)quotient(pair, shape.groups)), group0 = __builtin_amdgcn_readfirstlane((int)(pair - (int64_t)kvh * shape.groups) * kRows);
+    const int pair = (int)((uint32_t)(t - base) / (uint32_t)shape.tiles);
+    const int tile0 = __builtin_amdgcn_readfirstlane(t - base - pair * shape.tiles);
+    const int tile1 = __builtin_amdgcn_readfirstlane(min(shape.tiles, tile0 + (t_end - t)));
+    const int kvh = __builtin_amdgcn_readfirstlane((int)((uint32_t)pair / (uint32_t)shape.groups)), group0 = __builtin_amdgcn_readfirstlane((pair - kvh * shape.groups) * kRows);
     t += tile1 - tile0;
 
     // ---- rows ----
@@ -209,7 +258,7 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
     }
     const int hi_max = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)(min(group0 + kRows, n_list) - 1) / a.group_div));
     const int hi_min = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)group0 / a.group_div));
-    const int key_end = __builtin_amdgcn_readfirstlane(min((int)min((int64_t)tile1 * (int)tile.d, (int64_t)INT32_MAX), hi_max + 1));
+    const int key_end = __builtin_amdgcn_readfirstlane(min((int)min((int64_t)tile1 << tile_bits, (int64_t)INT32_MAX), hi_max + 1));
 
     bool odd = false;                                   // this lane has left out an infinity or NaN of V
     f32x4 acc[kNT][kAcc];
@@ -235,7 +284,7 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
       k_lane[i] = key * row_bytes + (place ^ (key & 15)) * 16;
     }
     const uint32_t v_lane = key_lane * row_bytes + place * 16;
-    const char* const k_ring = ring + wave * 2 * kHalf, * const v_ring = k_ring + kHalf;
+    char* const k_ring = ring + wave * 2 * kHalf, * const v_ring = k_ring + kHalf;
     const int32_t* const table = c.table + seq * c.table_stride;
 
     // Steps of this wavefront, kKeys keys each: step i takes keys key_of(i) .. + kKeys.  A refill looks up the pages of the next 64
@@ -245,7 +294,7 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
       uint32_t here;                                    // bit b: block b lies in this pool
       int64_t at[kBlocks];                              // where the blocks lie, in bytes
     };
-    auto key_of = [&](int i) { return tile0 * (int)tile.d + (i * kWaves + wave) * kKeys; };
+    auto key_of = [&](int i) { return (tile0 << tile_bits) + (i * kWaves + wave) * kKeys; };
     int ahead = 0, pages = 0;                           // first step of the refill; page of this lane's block
     uint64_t todo = 0;                                  // blocks of the refill that are here and not fetched
     auto refill = [&] {
@@ -285,10 +334,10 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
         for (int i = 0; i < kBlockCopies; ++i)
           copy_past_caches(v_head + x.at[b] + (int64_t)i * (64 / kRowChunks) * row_bytes, v_lane, ring, wave * 2 * kHalf + kHalf + (b * kBlockCopies + i) * 1024);
     };
-    // edge: the step has keys that some rows see and others do not.  The step's copies are on their way, K's before V's; the following step's K is asked for as soon as this
+    // The step's copies are on their way, K's before V's; the following step's K is asked for as soon as this
     // one's has been read, and so is V.
-    auto compute = [&](const Step& x, auto edge, auto has_next, const Step& after) {
-      const bool whole = !decltype(edge)::value && x.k0 + kKeys - 1 <= hi_max && x.here == (1u << kBlocks) - 1;   // every row sees every key
+    auto compute = [&](const Step& x, bool more, const Step& after) {
+      const bool whole = x.k0 + kKeys - 1 <= hi_min && x.here == (1u << kBlocks) - 1;   // every row sees every key of the step
 
       wait_copies<kCopies>();                            // V's may be under way
       u32x4 k[kBlocks][kKL];
@@ -296,7 +345,7 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int i = 0; i < kKL; ++i) k[b][i] = *reinterpret_cast<const u32x4*>(k_ring + (b * 16 + col) * kD * kElt + ((i * 4 + quad) ^ col) * 16);
-      if constexpr (decltype(has_next)::value) {
+      if (more) {
         wait_reads();
         copy_k(after);
       }
@@ -366,75 +415,84 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
           p_lo[j] = __builtin_bit_cast(bf16x8, mk4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]));
         }
       }
-      // What no row sees is not to be multiplied, not even by zero: it may be anything.  Nor is an infinity or NaN that some rows see and others do
-      // not (some_too): it is left out here and added to the rows that see it after the loop.
-      constexpr int kMasks = 4;                          // bf16: pairs of keys; f32: keys
-      uint32_t seen[kMasks], some[kMasks];
+      if (more) wait_copies<kCopies>();                  // the next step's K is under way
+      else wait_copies<0>();
+      char* const v_mine = v_ring + quad * 4 * kD * kElt + col * 16;   // what this lane reads of V: rows 16 b + r from here, pieces 16 e
+      if (!whole) {
+        // What no row sees is not to be multiplied, not even by zero: it may be anything.
 #pragma unroll
-      for (int y = 0; y < kMasks; ++y) {
-        const int key = kBf16 ? x.k0 + 16 * (y >> 1) + quad * 4 + (y & 1) * 2 : x.k0 + quad * 4 + y;
-        const int b = kBf16 ? y >> 1 : 0;
-        const bool in = x.here >> b & 1;
-        auto bits = [](bool first, bool second) { return kBf16 ? (first ? 0xffffu : 0u) | (second ? 0xffff0000u : 0u) : first ? ~0u : 0u; };
-        seen[y] = bits(in && key <= hi_max, in && key + 1 <= hi_max);
-        some[y] = bits(key > hi_min, key + 1 > hi_min);
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!(x.here >> b & 1) || x.k0 + 16 * b + quad * 4 + r > hi_max)
+#pragma unroll
+              for (int e = 0; e < kVC; ++e) *reinterpret_cast<u32x4*>(v_mine + (b * 16 + r) * kD * kElt + e * 256) = mk4(0u, 0u, 0u, 0u);
+        // Nor is an infinity or NaN that some rows see and others do not: it is left out here and added to the rows that see it after the loop.
+        if (hi_min < hi_max && x.k0 + kKeys - 1 > hi_min) {
+#pragma unroll 1
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int e = 0; e < kVC; ++e) {
+                u32x4* const at = reinterpret_cast<u32x4*>(v_mine + (b * 16 + r) * kD * kElt + e * 256);
+                const u32x4 y = *at;
+                u32x4 fine;
+                bool left_out = false;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                  fine[w] = finite_part<kBf16>(y[w]);
+                  left_out = left_out || fine[w] != y[w];
+                }
+                if (left_out && x.k0 + 16 * b + quad * 4 + r > hi_min) {
+                  *at = fine;
+                  odd = true;
+                }
+              }
+        }
       }
-      wait_copies<decltype(has_next)::value ? kCopies : 0>();   // K's of the next step may be under way
       u32x4 v[kBlocks][4][kVC];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int e = 0; e < kVC; ++e) v[b][r][e] = *reinterpret_cast<const u32x4*>(v_ring + (b * 16 + quad * 4 + r) * kD * kElt + (e * 16 + col) * 16);
-      if constexpr (decltype(has_next)::value) {
+          for (int e = 0; e < kVC; ++e) v[b][r][e] = *reinterpret_cast<const u32x4*>(v_mine + (b * 16 + r) * kD * kElt + e * 256);
+      if (more) {
         wait_reads();
         copy_v(after);
       }
-      auto add_pv = [&](auto some_too) {
-        auto word = [&](uint32_t w, int y) {
-          w &= seen[y];
-          if constexpr (decltype(some_too)::value) {
-            const uint32_t left_out = (w ^ finite_part<kBf16>(w)) & some[y];
-            odd = odd || left_out != 0;
-            w ^= left_out;
-          }
-          return w;
-        };
 #pragma unroll
-        for (int e = 0; e < kAcc; ++e) {
-          bf16x8 va = {};
-          float vf[4] = {};
-          if constexpr (kBf16) {                         // d = 8 (row of A) + e
-            const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
-            uint32_t w[4];
+      for (int e = 0; e < kAcc; ++e) {
+        bf16x8 va = {};
+        float vf[4] = {};
+        if constexpr (kBf16) {                         // d = 8 (row of A) + e
+          const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
+          uint32_t w[4];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) w[y] = word(__builtin_amdgcn_perm(v[y >> 1][(y & 1) * 2 + 1][0][e >> 1], v[y >> 1][(y & 1) * 2][0][e >> 1], pick), y);
-            va = __builtin_bit_cast(bf16x8, mk4(w[0], w[1], w[2], w[3]));
-          } else {                                       // d = 64 (e / 4) + 4 (row of A) + e % 4
+          for (int y = 0; y < 4; ++y) w[y] = __builtin_amdgcn_perm(v[y >> 1][(y & 1) * 2 + 1][0][e >> 1], v[y >> 1][(y & 1) * 2][0][e >> 1], pick);
+          va = __builtin_bit_cast(bf16x8, mk4(w[0], w[1], w[2], w[3]));
+        } else {                                       // d = 64 (e / 4) + 4 (row of A) + e % 4
 #pragma unroll
-            for (int y = 0; y < 4; ++y) vf[y] = __uint_as_float(word(v[0][y][e / 4][e % 4], y));
-          }
+          for (int y = 0; y < 4; ++y) vf[y] = __uint_as_float(v[0][y][e / 4][e % 4]);
+        }
 #pragma unroll
-          for (int j = 0; j < kNT; ++j) {
-            if constexpr (kBf16) {
-              acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_hi[j], acc[j][e], 0, 0, 0);
-              acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_lo[j], acc[j][e], 0, 0, 0);
-            } else {
+        for (int j = 0; j < kNT; ++j) {
+          if constexpr (kBf16) {
+            acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_hi[j], acc[j][e], 0, 0, 0);
+            acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_lo[j], acc[j][e], 0, 0, 0);
+          } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i], p[j][0][i], acc[j][e], 0, 0, 0);
-            }
+            for (int i = 0; i < 4; ++i) acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i], p[j][0][i], acc[j][e], 0, 0, 0);
           }
         }
-      };
-      add_pv(edge);
+      }
     };
     // Wait for Q here, once: left to the compiler the wait would stand in the loop, where the same counter holds the copies.
 #pragma unroll
     for (int j = 0; j < kNT; ++j)
 #pragma unroll
       for (int i = 0; i < kKL; ++i) asm volatile("" : "+v"(q[j][i]));
-    auto on_edge = [&](const Step& x) { return hi_min < hi_max && x.k0 + kKeys - 1 > hi_min; };   // the last steps, where rows differ in what they see
     Step now, after;
     if (key_of(0) < key_end) refill();
     bool have = next(now);
@@ -442,23 +500,13 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
       copy_k(now);
       copy_v(now);
     }
-    while (have && !on_edge(now)) {
+    while (have) {
       have = next(after);
-      if (have) compute(now, std::false_type(), std::true_type(), after);
-      else compute(now, std::false_type(), std::false_type(), now);
+      compute(now, have, after);
       now = after;
     }
-    while (have) {
-      compute(now, std::true_type(), std::false_type(), now);
-      have = next(now);
-      if (have) {
-        wait_reads();
-        copy_k(now);
-        copy_v(now);
-      }
-    }
     if (__any(odd)) {
-      for (int key = max(tile0 * (int)tile.d, hi_min + 1); key < key_end; ++key) {
+      for (int key = max((tile0 << tile_bits), hi_min + 1); key < key_end; ++key) {
         const int tp = (int)((uint32_t)key / c.page_div), page = table[tp];
         if (page < 0 || page >= c.n_pages) continue;
         const char* const row = v_head + (page * c.page_stride + (key - tp * c.page_size) * c.tok_stride) * kElt;
@@ -541,7 +589,7 @@ __global__ __launch_bounds__(64 * waves_of<kNT>(), kNT == 1 ? 2 : 1) void cache_
 // results.  It is a chain of latencies: which sequence and which partial results, these with their maxima and sums, the result.  All that one
 // of them needs is asked for at once: 28 workgroups that join 128 partial results each took 10.8 us with maxima, sums and results after one another, and take XX.
 template <bool kBf16, int kD, int kRows>
-__global__ __launch_bounds__(256, JO) void cache_join_kernel(CacheAttnArgs a, int n_groups, FastDiv tile, Partial part) {
+__global__ __launch_bounds__(256, JO) void cache_join_kernel(CacheAttnArgs a, int n_groups, Partial part) {
   constexpr int kTeam = kD / 4, kTeams = 256 / kTeam, kBatch = JB;
   __shared__ f32x4 xs[kTeams][kTeam];
   __shared__ float ls[kTeams], tops[4], ms[kMaxGroups], sums[kMaxGroups];
@@ -565,12 +613,12 @@ __global__ __launch_bounds__(256, JO) void cache_join_kernel(CacheAttnArgs a, in
   if (seq < 0 || seq >= c.n_seqs) return;
   const SeqRows r = rows_of_seq(c, seq);
   if (row < r.first || row - r.first >= r.count) return;
-  const PairShape shape = pairs_of<kRows>(a, r, tile);
   const int kvh = (int)((uint32_t)h / a.group_div), i = (row - r.first) * a.group + h - kvh * a.group, jr = i % kRows;
-  const int64_t total = part.prefix[c.n_seqs], t0 = part.prefix[seq] + ((int64_t)kvh * shape.groups + i / kRows) * shape.tiles;
-  const int64_t each = tiles_each(total, n_groups);
-  const int w0 = (int)quotient(t0, each), count = (int)quotient(t0 + shape.tiles - 1, each) - w0 + 1;
-  if (count == 1) return;                               // finished where it was computed
+  const int tile_bits = part.prefix[c.n_seqs + 1];
+  const PairShape shape = pairs_of<kRows>(a, r, tile_bits);
+  const int t0 = part.prefix[seq] + (kvh * shape.groups + i / kRows) * shape.tiles, each = tiles_each(part.prefix[c.n_seqs], n_groups);
+  const int w0 = (int)((uint32_t)t0 / (uint32_t)each), count = (int)((uint32_t)(t0 + shape.tiles - 1) / (uint32_t)each) - w0 + 1;
+  if (count <= 1 || t0 < 0 || w0 + count > n_groups) return;   // finished where it was computed (or cu_new is not ascending)
   const int team = tid / kTeam, e = tid % kTeam;
   auto at = [&](int s) { return (2 * (int64_t)(w0 + s) + (s == 0 ? 1 : 0)) * kRows + jr; };
   f32x4 y[kBatch];
@@ -630,21 +678,24 @@ __global__ __launch_bounds__(256, JO) void cache_join_kernel(CacheAttnArgs a, in
   if (a.lse != nullptr && e == 0) a.lse[h * a.lse_hs + row] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// How a call is laid out: tiles of 16 rows of a workgroup's group, workgroups, keys of a tile, and whether several workgroups may share a pair.
-struct Plan { int nt, groups, tile; bool shared; };
-Plan plan_of(const CacheAttnArgs& a) {
+// How a call is laid out: tiles of 16 rows of a workgroup's group, wavefronts of a workgroup, workgroups, the logarithm of a tile's keys (-1: picked by the kernel), and whether several workgroups may
+// share a pair.
+struct Plan { int nt, waves, groups, tile_bits; bool shared; double most; };   // most: tiles of all pairs at most
+Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   const CacheArgs& c = a.cache;
-  // As many rows as a sequence has on average in one group, up to 48: every further group reads the keys again.
-  const int64_t mean = ((int64_t)c.n_rows * a.group + c.n_seqs - 1) / c.n_seqs;
+  // The rows of a sequence in one group, up to 48: every further group reads the keys again.  With ragged numbers of new tokens, twice the mean.
+  const int64_t rows_each = c.cu_new == nullptr ? a.group : 2 * ((int64_t)c.n_rows * a.group / c.n_seqs);
   Plan p;
-  p.nt = mean <= 16 ? 1 : mean <= 32 ? 2 : 3;
-  const int round = kRound * (p.nt == 1 ? waves_of<1>() : waves_of<2>());
-  const int64_t rows = 16 * p.nt, capacity = (int64_t)c.max_pages * c.page_size, rounds = std::max<int64_t>(1, (capacity + round - 1) / round);
-  // A cache of a few rounds: one workgroup for a pair, and no second launch.
-  p.shared = rounds > kWholeRounds;
-  p.tile = p.shared ? round : (int)rounds * round;
-  const int64_t pairs = ((int64_t)c.n_rows * a.group / rows + c.n_seqs) * a.Hkv, room = std::min(kMaxGroups, cu_count());
-  p.groups = (int)std::min(room, std::min(pairs, room) * (p.shared ? rounds : 1));
+  p.nt = rows_each <= 16 ? 1 : rows_each <= 32 ? 2 : 3;
+  const int64_t capacity = (int64_t)c.max_pages * c.page_size;
+  const double pairs = (double)((int64_t)c.n_rows * a.group / (16 * p.nt) + c.n_seqs) * a.Hkv;
+  // A cache of a few steps: one workgroup for a pair, of eight wavefronts where the chip has a CU for each, and no second launch.
+  auto whole = [&](int waves) { return kWholeSteps * (bf16 ? 32 : 16) * waves; };
+  p.waves = p.nt == 1 && pairs <= cu_count() && capacity <= whole(8) ? 8 : 4;
+  p.shared = capacity > whole(p.waves);
+  p.tile_bits = p.shared ? -1 : 30;
+  p.most = pairs * (p.shared ? (double)((capacity + (bf16 ? 127 : 63)) / (bf16 ? 128 : 64)) : 1.);
+  p.groups = (int)std::min<double>(std::min(kMaxGroups, cu_count() * (p.waves == 4 && p.nt <= 2 ? 2 : 1)), p.most);
   return p;
 }
 
@@ -652,38 +703,39 @@ int64_t align16(int64_t x) { return (x + 15) / 16 * 16; }
 
 }  // namespace
 
+double cache_attn_tiles(const CacheAttnArgs& a, int io_dtype) { return plan_of(a, io_dtype == 0).most; }
+
 int64_t cache_attn_workspace_bytes(const CacheAttnArgs& a, int io_dtype) {
-  (void)io_dtype;
-  const Plan p = plan_of(a);
-  return align16(8 * ((int64_t)a.cache.n_seqs + 1)) + (int64_t)2 * p.groups * 16 * p.nt * 4 * (2 + a.d);
+  const Plan p = plan_of(a, io_dtype == 0);
+  return align16(4 * ((int64_t)a.cache.n_seqs + 2)) + (int64_t)2 * p.groups * 16 * p.nt * 4 * (2 + a.d);
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t stream) {
   if (a.cache.n_rows == 0 || a.cache.n_seqs == 0) return hipSuccess;
-  const Plan p = plan_of(a);
+  const Plan p = plan_of(a, io_dtype == 0);
   Partial part;
   char* w = a.ws;
-  part.prefix = reinterpret_cast<int64_t*>(w);
-  w += align16(8 * ((int64_t)a.cache.n_seqs + 1));
+  part.prefix = reinterpret_cast<int32_t*>(w);
+  w += align16(4 * ((int64_t)a.cache.n_seqs + 2));
   const int64_t rows = (int64_t)2 * p.groups * 16 * p.nt;
   part.o = reinterpret_cast<float*>(w);
   part.m = part.o + rows * a.d;
   part.l = part.m + rows;
-  auto launch = [&](auto bf16, auto d, auto nt) {
+  auto launch = [&](auto bf16, auto d, auto nt, auto waves) {
     constexpr bool kBf16 = decltype(bf16)::value;
-    constexpr int kD = decltype(d)::value, kNT = decltype(nt)::value;
-    cache_attn_kernel<kBf16, kD, kNT><<<dim3((unsigned)p.groups), dim3(64 * waves_of<kNT>()), 0, stream>>>(a, p.groups, fast_div(p.tile), part);
+    constexpr int kD = decltype(d)::value, kNT = decltype(nt)::value, kWaves = decltype(waves)::value;
+    cache_attn_kernel<kBf16, kD, kNT, kWaves><<<dim3((unsigned)p.groups), dim3(64 * kWaves), 0, stream>>>(a, p.groups, p.tile_bits, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.shared || p.groups == 1) return e;
-    cache_join_kernel<kBf16, kD, 16 * kNT><<<dim3((unsigned)((int64_t)a.cache.n_rows * a.Hq)), dim3(256), 0, stream>>>(a, p.groups, fast_div(p.tile), part);
+    cache_join_kernel<kBf16, kD, 16 * kNT><<<dim3((unsigned)((int64_t)a.cache.n_rows * a.Hq)), dim3(256), 0, stream>>>(a, p.groups, part);
     return hipGetLastError();
   };
   auto by_rows = [&](auto bf16, auto d) {
-    switch (p.nt) {
-      case 1: return launch(bf16, d, std::integral_constant<int, 1>());
-      case 2: return launch(bf16, d, std::integral_constant<int, 2>());
-      default: return launch(bf16, d, std::integral_constant<int, 3>());
-    }
+    using four = std::integral_constant<int, 4>;
+    if (p.nt == 3) return launch(bf16, d, std::integral_constant<int, 3>(), four());
+    if (p.nt == 2) return launch(bf16, d, std::integral_constant<int, 2>(), four());
+    if (p.waves == 4) return launch(bf16, d, std::integral_constant<int, 1>(), four());
+    return launch(bf16, d, std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
   };
   if (io_dtype == 0) return by_rows(std::true_type(), std::integral_constant<int, 128>());
   if (a.d == 128) return by_rows(std::false_type(), std::integral_constant<int, 128>());
