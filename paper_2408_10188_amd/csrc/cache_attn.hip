@@ -1,17 +1,22 @@
 // Attention of new tokens over a paged key-value cache: every K and V row is read once for the handful of query rows that
-// share its KV head, so the memory rate bounds it (28/4 heads, one token: 7 of the 16 columns of a matrix instruction, 3.5 flops a byte).
+// share its KV head, so the memory rate bounds it (28/4 heads, one token: 7 of the 16 columns of a matrix instruction, 7 flops a byte).
 //
 // Work.  The (token, head) pairs of a KV head's new rows are one list, as in the forward kernel; groups of kRows of it are
-// stationary.  A pair of (sequence, KV head, group) has ceil(length / 128) tiles of 128 keys.  The tiles of all pairs are one sequence that is cut
+// stationary.  A pair of (sequence, KV head, group) has the sequence's keys in tiles.  The tiles of all pairs are one sequence that is cut
 // into as many equal ranges as there are workgroups, whatever the lengths are: a workgroup goes through the segments
 // of pairs in its range.  A pair inside one range is finished there; at most the first and the last segment of a range are
 // parts of pairs that others share: their (O, maximum, sum) goes to the workspace and a second launch joins them.  The lengths are on the device only,
 // so each workgroup adds up the tiles of all sequences for itself.
 //
-// Wavefronts.  The four wavefronts of a workgroup take different keys and meet when a segment ends, so the loop has no barrier and
-// no LDS.  S^T = K . Q^T: K rows are A operands as they lie in memory.  O^T += V^T . P^T: the 16 keys of a block are dealt to the contraction
+// Wavefronts.  Those of a workgroup take different keys, 32 (f32: 16) a step, and meet when a segment ends, so the loop has no barrier: each
+// has LDS of its own for K and V of one step, and asks for the next step's K as soon as it has read this one's, and so for V.  The copies are asynchronous, and
+// their waits written out, as in the forward (loads into registers were moved together, ahead of their waits, by the compiler: 69 instead of 64 us for 64
+// ragged sequences).  S^T = K . Q^T, O^T += V^T . P^T: the 16 keys of a block are dealt to the contraction
 // slots so that the accumulators of S^T are B operands as they are, and a lane's V pieces (8 elements of d of the 8 keys of its
-// slots, each row read as 256 contiguous bytes by 16 lanes) become the A operands of 8 products by exchanging halves of registers.
+// slots) become the A operands of 8 products by exchanging halves of registers.
+//
+// Measured, 28/4 heads, one token, both launches: 203 tokens 6.8 us (a chain: lengths, pages and Q, K and V, the results), 256K tokens 87 us, of which the loop reads
+// 6.9 TB/s (a plain read of that size 7.1), 64 sequences of 150 to 16384 tokens 67 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -23,20 +28,6 @@ namespace {
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
-#ifndef JB
-#define JB 4
-#endif
-#ifndef JO
-#define JO 8
-#endif
-#ifndef WR
-#define WR 4
-#endif
-#ifndef MS
-#define MS 8
-#endif
-constexpr int kWholeSteps = WR;
-constexpr int kMostSplit = MS;
 constexpr int kMaxGroups = 1024;                        // workgroups of a launch
 
 struct Partial {
@@ -102,8 +93,12 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
 // Tiles of a workgroup's range: workgroup w has tiles [w * each, (w + 1) * each) of `total`.  (The host has made sure that there are fewer than 2^31.)
 __device__ __forceinline__ int tiles_each(int total, int n_groups) { return max(1, (int)(((uint32_t)total + n_groups - 1) / (uint32_t)n_groups)); }
 
-// Keys of a tile, as a logarithm: the fewest, from a step of four wavefronts on, with which every workgroup has at most one tile, or else kMostSplit, the one with the least waste where workgroups
-// go through several segments.  tiles(bits): those of this lane's sequence.
+// Keys of a tile, as a logarithm: the fewest, from a step of four wavefronts on, with which every workgroup has at most one tile, or else 256.  Smaller tiles
+// balance better, but each segment of a range costs some 4 us (28/4 heads, 64 sequences of 150 to 16384 tokens, tiles of 64 / 128 / 256 / 512 keys: 66.9 / 64.5 /
+// 62.8 / 62.6 us; 16 drafts of up to five tokens on 40 to 5003: 36 / 26 / 22.8; five f32 sequences of 1 to 1001: 5.7 / 6.6 / 8.8).
+// tiles(bits): those of this lane's sequence.
+constexpr int kUsualBits = 8;
+constexpr int fewest_bits(bool bf16) { return bf16 ? 7 : 6; }
 template <int kFewest, class Tiles>
 __device__ __forceinline__ int pick_tile(Tiles tiles, int n_groups) {
   constexpr int kMost = 9;
@@ -114,14 +109,14 @@ __device__ __forceinline__ int pick_tile(Tiles tiles, int n_groups) {
   for (int w = 1; w < 64; w <<= 1)
 #pragma unroll
     for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] += __shfl_xor(n[b - kFewest], w);
-  int bits = kMostSplit;
+  int bits = kUsualBits;
 #pragma unroll
   for (int b = kMost; b >= kFewest; --b) bits = n[b - kFewest] <= n_groups ? b : bits;
   return __builtin_amdgcn_readfirstlane(bits);
 }
 
 template <bool kBf16, int kD, int kNT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kNT <= 2 ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a, int n_groups, int tile_bits, Partial part) {
+__global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArgs a, int n_groups, int tile_bits, Partial part) {
   constexpr int kThreads = 64 * kWaves;
   constexpr int kRows = 16 * kNT, kElt = kBf16 ? 2 : 4;
   constexpr int kBlocks = kBf16 ? 2 : 1, kKeys = 16 * kBlocks;   // blocks of 16 keys, keys of a step
@@ -152,7 +147,7 @@ __global__ __launch_bounds__(64 * kWaves, kNT <= 2 ? 2 : 1) void cache_attn_kern
   int t, t_end, seq, base;                              // the next tile, the range's end; the tile's sequence, and tiles before that one
   if (few) {
     if (lane < c.n_seqs) mine = rows_of_seq(c, lane);
-    if (tile_bits < 0) tile_bits = pick_tile<kBf16 ? 7 : 6>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, n_groups);
+    if (tile_bits < 0) tile_bits = pick_tile<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, n_groups);
     const int n = lane < c.n_seqs ? tiles_of(mine, tile_bits) : 0;
     int upto = n;
 #pragma unroll
@@ -172,7 +167,7 @@ __global__ __launch_bounds__(64 * kWaves, kNT <= 2 ? 2 : 1) void cache_attn_kern
     seq = 63 - __builtin_clzll(__ballot(lane < c.n_seqs && upto - n <= t) | 1);   // the last one that begins by then
     base = __builtin_amdgcn_readlane(upto - n, seq);
   } else {
-    if (tile_bits < 0) tile_bits = kMostSplit;
+    if (tile_bits < 0) tile_bits = kUsualBits;
     const int per = (c.n_seqs + kThreads - 1) / kThreads, s_first = min(tid * per, c.n_seqs), s_last = min(s_first + per, c.n_seqs);
     int n = 0;
     for (int s = s_first; s < s_last; ++s) n += tiles_of(rows_of_seq(c, s), tile_bits);
@@ -488,13 +483,14 @@ __global__ __launch_bounds__(64 * kWaves, kNT <= 2 ? 2 : 1) void cache_attn_kern
         }
       }
     };
-    // Wait for Q here, once: left to the compiler the wait would stand in the loop, where the same counter holds the copies.
+    Step now, after;
+    if (key_of(0) < key_end) refill();
+    // Q has landed too, since it was asked for before the pages.  Left to the compiler the wait for it would stand in the loop, where the same counter
+    // holds the copies.
 #pragma unroll
     for (int j = 0; j < kNT; ++j)
 #pragma unroll
       for (int i = 0; i < kKL; ++i) asm volatile("" : "+v"(q[j][i]));
-    Step now, after;
-    if (key_of(0) < key_end) refill();
     bool have = next(now);
     if (have) {
       copy_k(now);
@@ -587,10 +583,11 @@ __global__ __launch_bounds__(64 * kWaves, kNT <= 2 ? 2 : 1) void cache_attn_kern
 
 // Joins the partial results of pairs that several workgroups shared.  A workgroup takes one (row, head); teams of d / 4 threads share out the partial
 // results.  It is a chain of latencies: which sequence and which partial results, these with their maxima and sums, the result.  All that one
-// of them needs is asked for at once: 28 workgroups that join 128 partial results each took 10.8 us with maxima, sums and results after one another, and take XX.
+// of them needs is asked for at once: 28 workgroups that join 128 partial results each took
+// 10.8 us with maxima, sums and results after one another, and take 6.1 (64 partial results: 4.9).
 template <bool kBf16, int kD, int kRows>
-__global__ __launch_bounds__(256, JO) void cache_join_kernel(CacheAttnArgs a, int n_groups, Partial part) {
-  constexpr int kTeam = kD / 4, kTeams = 256 / kTeam, kBatch = JB;
+__global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, int n_groups, Partial part) {
+  constexpr int kTeam = kD / 4, kTeams = 256 / kTeam, kBatch = 4;
   __shared__ f32x4 xs[kTeams][kTeam];
   __shared__ float ls[kTeams], tops[4], ms[kMaxGroups], sums[kMaxGroups];
   __shared__ int before[4];
@@ -678,24 +675,30 @@ __global__ __launch_bounds__(256, JO) void cache_join_kernel(CacheAttnArgs a, in
   if (a.lse != nullptr && e == 0) a.lse[h * a.lse_hs + row] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// How a call is laid out: tiles of 16 rows of a workgroup's group, wavefronts of a workgroup, workgroups, the logarithm of a tile's keys (-1: picked by the kernel), and whether several workgroups may
-// share a pair.
+// How a call is laid out: tiles of 16 rows of a workgroup's group, wavefronts of a workgroup, workgroups, the logarithm of a tile's keys (-1: picked by the
+// kernel), and whether several workgroups may share a pair.
 struct Plan { int nt, waves, groups, tile_bits; bool shared; double most; };   // most: tiles of all pairs at most
 Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   const CacheArgs& c = a.cache;
-  // The rows of a sequence in one group, up to 48: every further group reads the keys again.  With ragged numbers of new tokens, twice the mean.
+  const int n_cu = cu_count();
+  // The rows of a sequence in one group where 32 hold them: every further group reads the keys again.  With ragged numbers of new tokens, twice the mean.
+  // (Groups of 48 rows, one workgroup a CU: 28/4 heads, 5 new tokens on 65536: 37.8 instead of 43.7 us, 16 new ones 82.3 instead of 61.2.)
   const int64_t rows_each = c.cu_new == nullptr ? a.group : 2 * ((int64_t)c.n_rows * a.group / c.n_seqs);
   Plan p;
-  p.nt = rows_each <= 16 ? 1 : rows_each <= 32 ? 2 : 3;
+  p.nt = rows_each <= 16 ? 1 : 2;
   const int64_t capacity = (int64_t)c.max_pages * c.page_size;
   const double pairs = (double)((int64_t)c.n_rows * a.group / (16 * p.nt) + c.n_seqs) * a.Hkv;
-  // A cache of a few steps: one workgroup for a pair, of eight wavefronts where the chip has a CU for each, and no second launch.
-  auto whole = [&](int waves) { return kWholeSteps * (bf16 ? 32 : 16) * waves; };
-  p.waves = p.nt == 1 && pairs <= cu_count() && capacity <= whole(8) ? 8 : 4;
-  p.shared = capacity > whole(p.waves);
+  // A short cache: one workgroup for a pair, and no second launch.  28/4 heads, us so and with shared pairs: 8 sequences of 400 tokens 9.5 and 11.4, of
+  // 900 14.1 and 11.7; 60 of 900 21.4 and 27.7, 200 of 900 64.5 and 75.7, of 20 to 900 39.0 and 37.9, of 1900 138.0 and 138.9.
+  p.shared = capacity > (pairs * 2 >= n_cu ? 1024 : 512) / (bf16 ? 1 : 2);
+  // Eight wavefronts and a CU to itself, or four and half a CU.  Eight take a pair in half the time and leave half as many partial results (one sequence of 256K
+  // tokens: 87.2 instead of 89.7 us); of two workgroups on a CU one computes while the other starts or ends a segment (64 sequences of 150 to 16384: 68.8 instead
+  // of 63.2).
+  p.waves = p.nt == 1 && (p.shared ? pairs * 8 <= n_cu : pairs <= n_cu) ? 8 : 4;
   p.tile_bits = p.shared ? -1 : 30;
-  p.most = pairs * (p.shared ? (double)((capacity + (bf16 ? 127 : 63)) / (bf16 ? 128 : 64)) : 1.);
-  p.groups = (int)std::min<double>(std::min(kMaxGroups, cu_count() * (p.waves == 4 && p.nt <= 2 ? 2 : 1)), p.most);
+  const int fewest = 1 << fewest_bits(bf16);
+  p.most = pairs * (p.shared ? (double)((capacity + fewest - 1) / fewest) : 1.);
+  p.groups = (int)std::min<double>(std::min(kMaxGroups, n_cu * (p.waves == 4 ? 2 : 1)), p.most);
   return p;
 }
 
@@ -732,7 +735,6 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t s
   };
   auto by_rows = [&](auto bf16, auto d) {
     using four = std::integral_constant<int, 4>;
-    if (p.nt == 3) return launch(bf16, d, std::integral_constant<int, 3>(), four());
     if (p.nt == 2) return launch(bf16, d, std::integral_constant<int, 2>(), four());
     if (p.waves == 4) return launch(bf16, d, std::integral_constant<int, 1>(), four());
     return launch(bf16, d, std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
