@@ -21,7 +21,7 @@ def heads_of(t):
     """mmsp_heads of a tensor [rows, n_heads, d]."""
     if t.dim() != 3 or t.stride(2) != 1:
         raise ValueError("[rows, n_heads, d] with d contiguous is wanted")
-    return B.make_heads(t, t.shape[1], _io(t), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[2]), t.stride(1) if t.shape[1] > 1 else t.shape[2])
+    return B.make_heads(t, t.shape[1], _io(t), *_strides(t))
 
 
 def shape_for(k_pool, io_dtype, n_q_heads=None, n_rows=0, scale=1.0):
@@ -65,7 +65,7 @@ class PagedCache:
         self._refs, self._free = np.zeros(n_pages, dtype=np.int32), np.zeros(n_pages, dtype=np.int32)
         self.pages = B.make_pages(self._refs, self._free, page_size)
         self.rows, self.lengths, self._next = {}, {}, 0
-        self._step = None
+        self._step = self._ws = None
 
     def _add(self, row, length):
         self._next += 1
@@ -93,7 +93,8 @@ class PagedCache:
             return
         dev = torch.from_numpy(np.ascontiguousarray(copies, dtype=np.int32)).to(self.k.device)
         shape, cache = shape_for(self.k[0], _io(self.k)), cache_for(self.k[0], self.v[0])
-        B.mmsp_cache_copy_pages(shape, cache, len(self.k), self.k.stride(0), dev, len(copies), torch.cuda.current_stream(self.k.device).cuda_stream)
+        with torch.cuda.device(self.k.device):
+            B.mmsp_cache_copy_pages(shape, cache, len(self.k), self.k.stride(0), dev, len(copies), torch.cuda.current_stream().cuda_stream)
 
     def compact(self):
         """Moves the pages in use to the front of the pool; returns how many there are."""
@@ -120,7 +121,7 @@ class PagedCache:
                 done.append((s, n, before))
                 if copy is not None:
                     copies.append(copy)
-        except B.MmspError:
+        except Exception:
             for s, n, before in reversed(done):           # what was taken is given back
                 self._undo(s, n, before)
             raise
@@ -163,18 +164,22 @@ class PagedCache:
         cache, n = self._cache(layer), self._step[3]
         q_out = q if q_out is None else q_out
         for t in (q, k, v, q_out):
-            if t.shape[0] != n or t.dtype != self.k.dtype or t.stride(2) != 1:
-                raise ValueError("%d rows of %s with d contiguous are wanted" % (n, self.k.dtype))
+            if t.dim() != 3 or t.shape[0] != n or t.dtype != self.k.dtype or t.stride(2) != 1 or t.device != self.k.device:
+                raise ValueError("%d rows of %s with d contiguous, on the pool's device, are wanted" % (n, self.k.dtype))
         if _strides(k) != _strides(v) or k.shape != v.shape or q.shape != q_out.shape:
             raise ValueError("K and V must have the same shapes and strides, q_out Q's shape")
         if q_out.stride() != q.stride() if q_out.data_ptr() == q.data_ptr() else not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous, or q itself")
         if q.shape[1:] != (self.n_q_heads, self.k.shape[-1]) or k.shape[1:] != (self.k.shape[2], self.k.shape[-1]):
             raise ValueError("Q and K must have the cache's heads")
-        if rotary is not None and (positions.dtype != torch.int32 or positions.shape != (rotary.n_axes, n) or positions.stride(1) != 1):
-            raise ValueError("positions must be int32 [%d, %d]" % (rotary.n_axes, n))
-        B.mmsp_cache_append(self._shape(q, k), cache, rotary, positions, 0 if positions is None else max(n, positions.stride(0)), q, k, v, q_out,
-                            torch.cuda.current_stream(self.k.device).cuda_stream)
+        if rotary is not None and (positions is None or positions.dtype != torch.int32 or positions.shape != (rotary.n_axes, n) or positions.stride(1) != 1
+                                   or positions.device != self.k.device):
+            raise ValueError("positions must be int32 [%d, %d] on the pool's device" % (rotary.n_axes, n))
+        if n == 0:
+            return q_out
+        with torch.cuda.device(self.k.device):
+            B.mmsp_cache_append(self._shape(q, k), cache, rotary, positions, 0 if positions is None else max(n, positions.stride(0)), q, k, v, q_out,
+                                torch.cuda.current_stream().cuda_stream)
         return q_out
 
     def attend(self, layer, q, scale=None, o_final=None, o=None, lse=None):
@@ -182,17 +187,20 @@ class PagedCache:
         partial result (o, lse) for mmsp_attn_merge.  Dense [rows, n_q_heads, d] and [n_q_heads, rows]."""
         import torch
         cache, n = self._cache(layer), self._step[3]
-        if q.shape != (n, self.n_q_heads, self.k.shape[-1]) or q.dtype != self.k.dtype or q.stride(2) != 1:
-            raise ValueError("q must be %s [%d, %d, %d]" % (self.k.dtype, n, self.n_q_heads, self.k.shape[-1]))
+        if q.shape != (n, self.n_q_heads, self.k.shape[-1]) or q.dtype != self.k.dtype or q.stride(2) != 1 or q.device != self.k.device:
+            raise ValueError("q must be %s [%d, %d, %d] on the pool's device" % (self.k.dtype, n, self.n_q_heads, self.k.shape[-1]))
         if o_final is None and o is None:
             o_final = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         for t, dtype, size in ((o_final, q.dtype, tuple(q.shape)), (o, torch.float32, tuple(q.shape)), (lse, torch.float32, (self.n_q_heads, n))):
-            if t is not None and (t.dtype != dtype or tuple(t.shape) != size or not t.is_contiguous()):
-                raise ValueError("results must be contiguous, o_final in q's type, o and lse in float32")
+            if t is not None and (t.dtype != dtype or tuple(t.shape) != size or not t.is_contiguous() or t.device != q.device):
+                raise ValueError("results must be contiguous, on q's device, o_final in q's type, o and lse in float32")
+        if n == 0:
+            return o_final if o_final is not None else (o, lse)
         shape = self._shape(q, scale=q.shape[-1] ** -0.5 if scale is None else scale)
         if self._ws is None:                              # one for all layers of a step: they run one after the other
             self._ws = torch.empty(max(B.mmsp_cache_workspace_bytes(shape, cache), 16), dtype=torch.uint8, device=q.device)
-        B.mmsp_cache_attn(shape, cache, q, o_final, o, lse, self._ws, self._ws.numel(), torch.cuda.current_stream(self.k.device).cuda_stream)
+        with torch.cuda.device(q.device):
+            B.mmsp_cache_attn(shape, cache, q, o_final, o, lse, self._ws, self._ws.numel(), torch.cuda.current_stream().cuda_stream)
         return o_final if o_final is not None else (o, lse)
 
 

@@ -1,0 +1,124 @@
+"""The host side of the cache's Python layer, and that its structures are the header's.  No kernel is launched here."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2408_10188_amd import binding as B
+from paper_2408_10188_amd import paged
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_structures_are_laid_out_as_in_the_header(tmp_path):
+    structs = dict(mmsp_rotary=B.MmspRotary, mmsp_heads=B.MmspHeads, mmsp_cache=B.MmspCache, mmsp_page_copy=B.MmspPageCopy, mmsp_pages=B.MmspPages)
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "mmsp.h"', "int main(void) {"]
+    for name, s in structs.items():
+        lines.append('printf("%s %%zu\\n", sizeof(%s));' % (name, name))
+        lines += ['printf("%s.%s %%zu\\n", offsetof(%s, %s));' % (name, f, name, f) for f, _ in s._fields_]
+    (tmp_path / "a.c").write_text("\n".join(lines + ["return 0; }"]))
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-I", os.path.join(ROOT, "include"), str(tmp_path / "a.c"), "-o", str(tmp_path / "a")], check=True)
+    said = dict(ln.split() for ln in subprocess.run([str(tmp_path / "a")], check=True, capture_output=True, text=True).stdout.splitlines())
+    for name, s in structs.items():
+        assert int(said[name]) == ctypes.sizeof(s)
+        for f, _ in s._fields_:
+            assert int(said["%s.%s" % (name, f)]) == getattr(s, f).offset, (name, f)
+
+
+def _cache(n_pages=12, page=16, max_tokens=100):
+    return paged.PagedCache(2, n_pages, page, 4, 2, 128, max_tokens, torch.bfloat16, "cpu")
+
+
+def _state(c):
+    return c._refs.tolist(), c.pages.n_free, {s: r.tolist() for s, r in c.rows.items()}, dict(c.lengths)
+
+
+def test_steps_take_pages_all_or_none():
+    c = _cache()
+    a, b = c.add(), c.add()
+    c.step([a, b], [40, 16])
+    assert c.rows[a].tolist() == [0, 1, 2, -1, -1, -1, -1] and c.rows[b][:2].tolist() == [3, -1] and c.lengths == {a: 40, b: 16}
+    table, lengths, cu_new, n = c._step
+    assert table.tolist() == [c.rows[a].tolist(), c.rows[b].tolist()] and lengths.tolist() == [40, 16] and cu_new.tolist() == [0, 40, 56] and n == 56
+    c.step([b], [1])
+    assert c._step[2] is None and c.rows[b][:2].tolist() == [3, 4]
+    fork = c.fork(a)                                     # its last page is half full and shared
+    before = _state(c)
+    for seqs, n_new, error in (([b, fork, a], [64, 20, 60], B.MmspError), ([b, a], [70, 100], B.MmspError), ([fork, 99], [30, 1], KeyError),
+                               ([a, a], [1, 1], ValueError), ([a], [1, 2], ValueError), ([a], [-1], ValueError)):
+        with pytest.raises(error):
+            c.step(seqs, n_new)
+        assert _state(c) == before
+        assert sorted(c._free[:c.pages.n_free].tolist()) == [i for i, r in enumerate(before[0]) if r == 0]
+    c.free(a)
+    c.step([fork], [8])                                  # nobody else holds its last page any more: no copy is made
+    assert c.rows[fork][:3].tolist() == [0, 1, 2]
+    c.free(fork)
+    assert c.pages.n_free == 10 and sorted(np.flatnonzero(c._refs)) == [3, 4] and list(c.rows) == [b]
+    c.free(b)
+    assert c.pages.n_free == 12 and c.compact() == 0
+
+
+def test_compaction_of_an_empty_cache():
+    c = _cache()
+    assert c.compact() == 0
+    with pytest.raises(RuntimeError):
+        c.attend(0, torch.zeros(1, 4, 128, dtype=torch.bfloat16))
+
+
+def test_layers_of_the_python_side_refuse_wrong_tensors():
+    c = _cache()
+    a = c.add()
+    c.step([a], [3])
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    rot = B.mmsp_rotary_plan(128, 1e6, [16, 24, 24])
+    pos = torch.zeros(3, 3, dtype=torch.int32)
+    good = dict(q=bf(3, 4, 128), k=bf(3, 2, 128), v=bf(3, 2, 128), q_out=None)
+    wide = bf(3, 8, 128)
+    for kw in (dict(q=bf(2, 4, 128)), dict(q=bf(3, 5, 128)), dict(k=bf(3, 3, 128), v=bf(3, 3, 128)), dict(v=wide[:, :2]), dict(q=torch.zeros(3, 4, 128)), dict(q=wide[:, :4].to("meta")),
+               dict(q_out=wide[:, :4]), dict(q=wide[:, :4], q_out=wide.view(-1)[:3 * 512].view(3, 4, 128))):
+        with pytest.raises(ValueError):
+            c.append(0, rot, pos, **{**good, **kw})
+    for p in (None, pos[:2], pos.long(), torch.zeros(3, 4, dtype=torch.int32), pos.to("meta")):
+        with pytest.raises(ValueError):
+            c.append(0, rot, p, **good)
+    for kw in (dict(q=bf(3, 2, 128)), dict(o_final=torch.zeros(3, 4, 128)), dict(o=bf(3, 4, 128)), dict(o_final=wide[:, :4]), dict(lse=torch.zeros(4, 4)), dict(q=bf(3, 4, 128).to("meta"))):
+        with pytest.raises(ValueError):
+            c.attend(0, **{**dict(q=bf(3, 4, 128)), **kw})
+    pool = torch.zeros(4, 2, 16, 128)
+    for bad in (dict(v_pool=pool.bfloat16()), dict(v_pool=pool[:3]), dict(page_table=torch.zeros(1, 2)), dict(lengths=torch.zeros(1)),
+                dict(page_table=torch.zeros(2, 2, dtype=torch.int32), lengths=torch.zeros(1, dtype=torch.int32)),
+                dict(lengths=torch.zeros(2, dtype=torch.int32), cu_new=torch.zeros(2, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            paged.cache_for(**{**dict(k_pool=pool, v_pool=pool), **bad})
+    assert paged.heads_of(torch.zeros(3, 260, dtype=torch.bfloat16)[:1, :256].view(1, 2, 128)).tok_stride % 8 == 0
+    with pytest.raises(ValueError):
+        paged.heads_of(torch.zeros(3, 128, 4).transpose(1, 2))
+    with pytest.raises(ValueError):
+        paged.heads_of(torch.zeros(3, 4, 128, dtype=torch.float16))
+
+
+def test_a_step_without_tokens_does_nothing():
+    c = _cache()
+    a = c.add()
+    c.step([a], [0])
+    empty = torch.zeros(0, 4, 128, dtype=torch.bfloat16)
+    kv = torch.zeros(0, 2, 128, dtype=torch.bfloat16)
+    assert c.append(0, None, None, empty, kv, kv) is empty and c.attend(0, empty).shape == (0, 4, 128)
+    c.step([], [])
+
+
+def test_calls_too_large_for_a_grid_are_refused():
+    shape = B.make_shape(4, 2, 128, B.MMSP_BF16, 0.1, (512, 128), (256, 128), 1024)
+    cache = lambda n, pages: B.make_cache(4096, 4096, (4096, 128, 2048), 9, 16, 4096, pages, pages, n, 4096, None, n)
+    assert B.mmsp_cache_workspace_bytes(shape, cache(60, 1 << 26)) > 0
+    for n, pages in ((64, 1 << 26), (1 << 20, 1 << 17)):                    # 2^30 tokens each; 2^21, and a million sequences
+        with pytest.raises(B.MmspError) as e:
+            B.mmsp_cache_attn(B.make_shape(4, 2, 128, B.MMSP_BF16, 0.1, (512, 128), (256, 128), 1 << 20), cache(n, pages), 4096, 4096, None, None, 4096, 1 << 50)
+        assert e.value.status == B.MMSP_ERR_UNSUPPORTED
+    with pytest.raises(B.MmspError) as e:                                   # 2^22 layers of K and V of 512 pieces of 16 bytes: 2^32 threads
+        B.mmsp_cache_copy_pages(shape, cache(1, 1), 1 << 22, 8, 4096, 1)
+    assert e.value.status == B.MMSP_ERR_UNSUPPORTED
