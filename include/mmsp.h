@@ -323,7 +323,7 @@ typedef struct {
   int32_t n_seqs;
   const int32_t* lengths;    /* device, [n_seqs]: tokens of a sequence, its new ones included */
   const int32_t* cu_new;     /* device, [n_seqs + 1], ascending, or NULL                   */
-  int32_t n_rows;            /* rows that the row buffers have, <= 2^30                    */
+  int32_t n_rows;            /* rows that the row buffers have; it and n_seqs <= 2^26      */
 } mmsp_cache;
 
 /* New tokens into the cache: K turned by the rotary positions (rotary == NULL: as it is) and V are
@@ -343,12 +343,13 @@ size_t mmsp_cache_workspace_bytes(const mmsp_shape* shape, const mmsp_cache* cac
  * and query head
  *   S_j = softmax_scale * Q . K[token j]  over the tokens j <= the row's own whose page is in this pool,
  *   LSE = ln sum_j exp(S_j),  O = sum_j exp(S_j - LSE) V[token j].
- * A row that sees nothing, or only scores of -inf, gets O = 0, LSE = -inf; one with a NaN among its scores gets NaNs.  What lies in masked slots,
- * NaN or infinity included, has no influence.
+ * A row that sees nothing, or only scores of -inf, gets O = 0, LSE = -inf; one with a NaN or +inf among its scores gets NaNs.  What lies in masked slots,
+ * NaN or infinity included, has no influence.  A NaN in a V that a row sees gives a NaN in that element of O, an infinity gives an infinity or a NaN there.
  * q: [n_rows, n_q_heads, d] with the shape's q strides (its kv strides are not used).  Results, each may be NULL, not
  * all: o_final dense [n_rows, n_q_heads, d] in io_dtype; o the same in f32, for mmsp_attn_merge; lse
  * [n_q_heads][lse_head_stride].  Meant for one or a few new tokens per sequence (any number is right; a
- * whole prompt is faster through mmsp_attn_step_fwd).  Results are bit-identical from run to run on one kind of device.
+ * whole prompt is faster through mmsp_attn_step_fwd).  UNSUPPORTED where n_rows * n_q_heads exceeds 2^23, or
+ * sequences x KV heads x capacity (max_pages * page_size) some 2^36 tokens.  Results are bit-identical from run to run on one kind of device.
  * workspace: at least mmsp_cache_workspace_bytes() bytes, 16-byte aligned; its contents need not be set and
  * nothing in it outlives the call's kernels.  Calls that may overlap in time need one each. */
 mmsp_status mmsp_cache_attn(const mmsp_shape* shape, const mmsp_cache* cache, const void* q, void* o_final, float* o,

@@ -10,7 +10,7 @@ using namespace mmsp;
 
 namespace {
 
-constexpr int64_t kMaxRows = (int64_t)1 << 26;          // rows of a call: a grid has fewer than 2^32 threads
+constexpr int64_t kMaxRows = (int64_t)1 << 26;          // rows of a call
 
 mmsp_status check_rotary(const mmsp_rotary* r) {
   if (r == nullptr) return fail(MMSP_ERR_INVALID_ARG, "rotary is NULL");
@@ -214,7 +214,7 @@ mmsp_status mmsp_cache_attn(const mmsp_shape* shape, const mmsp_cache* cache, co
     return fail(MMSP_ERR_UNSUPPORTED, "%d rows x %d heads: more than 2^23 are not supported", cache->n_rows, shape->n_q_heads);
   if (cache->n_rows == 0 || cache->n_seqs == 0) return MMSP_OK;
   CacheAttnArgs a = attn_args(shape, cache);
-  if (cache_attn_tiles(a, shape->io_dtype) >= 0x1p31)
+  if (cache_attn_tiles(a, shape->io_dtype) > 0x1p30)
     return fail(MMSP_ERR_UNSUPPORTED, "%d sequences of up to %d pages of %d tokens and %d KV heads are too much for a call", cache->n_seqs, cache->max_pages,
                 cache->page_size, shape->n_kv_heads);
   const size_t need = (size_t)cache_attn_workspace_bytes(a, shape->io_dtype);
@@ -236,7 +236,7 @@ mmsp_status mmsp_cache_copy_pages(const mmsp_shape* shape, const mmsp_cache* cac
   if (n_copies > 0 && copies == nullptr) return fail(MMSP_ERR_INVALID_ARG, "copies is NULL");
   const int elt = shape->io_dtype == MMSP_BF16 ? 2 : 4;
   const double pieces = (double)cache->page_size * shape->n_kv_heads * shape->head_dim * elt / 16;
-  if (pieces > (1 << 28) || pieces * n_layers > 0x1p32)
+  if (pieces > (1 << 28) || pieces * 2 * n_layers >= 0x1p32)   // a grid has fewer than 2^32 threads
     return fail(MMSP_ERR_UNSUPPORTED, "pages of %d tokens x %d heads in %d layers are too large for a launch", cache->page_size, shape->n_kv_heads, n_layers);
   return device_result(launch_copy_pages(cache_args(cache), n_layers, layer_stride, shape->n_kv_heads, shape->head_dim, elt, reinterpret_cast<const int32_t*>(copies),
                                          n_copies, reinterpret_cast<hipStream_t>(hip_stream)),

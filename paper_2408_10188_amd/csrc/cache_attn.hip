@@ -66,12 +66,6 @@ __device__ __forceinline__ void store_row(void* to, int64_t at, const float (&x)
   }
 }
 
-// A value that is the same in all lanes, in scalar registers.
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
-  return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
 // Asynchronous copy of 64 x 16 bytes to LDS (see dma16), read once and so past the caches: 7.1 TB/s in a large plain read where the default policy
 // reaches 6.2.
 __device__ __forceinline__ void copy_past_caches(const char* base, uint32_t offset, const void* lds_array, int byte_offset) {
@@ -90,8 +84,11 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
   else return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
 }
 
-// Tiles of a workgroup's range: workgroup w has tiles [w * each, (w + 1) * each) of `total`.  (The host has made sure that there are fewer than 2^31.)
+// Tiles of a workgroup's range: workgroup w has tiles [w * each, (w + 1) * each) of `total`.  (The host has made sure that there are at most 2^30.)
 __device__ __forceinline__ int tiles_each(int total, int n_groups) { return max(1, (int)(((uint32_t)total + n_groups - 1) / (uint32_t)n_groups)); }
+
+// A sum that the host has ruled out comes from a cu_new that is not ascending: no tile is taken.
+__device__ __forceinline__ int checked_total(int total) { return total < 0 || total > 1 << 30 ? 0 : total; }
 
 // Keys of a tile, as a logarithm: the fewest, from a step of four wavefronts on, with which every workgroup has at most one tile, or else 256.  Smaller tiles
 // balance better, but each segment of a range costs some 4 us (28/4 heads, 64 sequences of 150 to 16384 tokens, tiles of 64 / 128 / 256 / 512 keys: 66.9 / 64.5 /
@@ -155,7 +152,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       const int x = __shfl_up(upto, w);
       if (lane >= w) upto += x;
     }
-    const int total = __builtin_amdgcn_readlane(upto, 63);
+    const int total = checked_total(__builtin_amdgcn_readlane(upto, 63));
     if (blockIdx.x == 0 && wave == 0) {                 // for the joining launch
       if (lane < c.n_seqs) part.prefix[lane] = upto - n;
       if (lane == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
@@ -186,7 +183,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       if (w < wave) upto += wave_tiles[w];
       total += wave_tiles[w];
     }
-    total = __builtin_amdgcn_readfirstlane(total);
+    total = checked_total(__builtin_amdgcn_readfirstlane(total));
     if (blockIdx.x == 0) {
       int x = upto - n;
       for (int s = s_first; s < s_last; ++s) { part.prefix[s] = x; x += tiles_of(rows_of_seq(c, s), tile_bits); }
@@ -615,7 +612,7 @@ __global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, int
   const PairShape shape = pairs_of<kRows>(a, r, tile_bits);
   const int t0 = part.prefix[seq] + (kvh * shape.groups + i / kRows) * shape.tiles, each = tiles_each(part.prefix[c.n_seqs], n_groups);
   const int w0 = (int)((uint32_t)t0 / (uint32_t)each), count = (int)((uint32_t)(t0 + shape.tiles - 1) / (uint32_t)each) - w0 + 1;
-  if (count <= 1 || t0 < 0 || w0 + count > n_groups) return;   // finished where it was computed (or cu_new is not ascending)
+  if (count <= 1 || t0 < 0 || w0 >= n_groups || count > n_groups - w0) return;   // finished where it was computed (or cu_new is not ascending)
   const int team = tid / kTeam, e = tid % kTeam;
   auto at = [&](int s) { return (2 * (int64_t)(w0 + s) + (s == 0 ? 1 : 0)) * kRows + jr; };
   f32x4 y[kBatch];

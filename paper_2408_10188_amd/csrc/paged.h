@@ -70,7 +70,7 @@ struct CacheAttnArgs {
   float scale;
   char* ws;
 };
-double cache_attn_tiles(const CacheAttnArgs& a, int io_dtype);   // tiles of work at most; 2^31 and more are for the caller to refuse
+double cache_attn_tiles(const CacheAttnArgs& a, int io_dtype);   // tiles of work at most; more than 2^30 are for the caller to refuse
 int64_t cache_attn_workspace_bytes(const CacheAttnArgs& a, int io_dtype);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t stream);
 

@@ -219,10 +219,11 @@ __global__ __launch_bounds__(256) void append_kernel(RotaryArgs rot, AppendArgs 
   }
 }
 
-// Rows of a workgroup: enough for the items that a thread has in flight, but not so many that CUs stay idle.
+// Rows of a workgroup: enough for the items that a thread has in flight, but not so many that CUs stay idle, nor so few that a grid of two such parts has 2^32 threads.
 int rows_of_group(int64_t n_rows, int heads, int vec, bool bf16) {
   const int64_t full = 256 * (bf16 ? items_of<true>() : items_of<false>()) / ((int64_t)heads * vec), spread = (n_rows + cu_count() - 1) / cu_count();
-  return (int)std::max<int64_t>(1, std::min<int64_t>({full, spread, kMaxRows}));
+  const int64_t least = (n_rows + (1 << 22) - 1) >> 22;  // 2^26 rows at most: 16
+  return (int)std::max<int64_t>({1, least, std::min<int64_t>({full, spread, kMaxRows})});
 }
 
 }  // namespace

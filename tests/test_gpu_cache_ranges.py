@@ -1,0 +1,69 @@
+"""The paged cache's calls at the ends of their ranges: page tables far wider than the sequences, more sequences than a workgroup's threads, rows in several
+groups with something in the keys that only the later ones see, and more rows than a grid has workgroups."""
+import math
+
+import pytest
+import torch
+
+from paper_2408_10188_amd import binding as B
+from paper_2408_10188_amd import paged
+from tests.helpers import DEV
+from tests.test_gpu_cache import BF16, F32, Problem
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("case", [dict(lengths=[1]), dict(lengths=[5, 0, 40]), dict(lengths=list(range(100)), hq=4, hkv=2), dict(lengths=[16, 2100], new=[2, 3]),
+                                  dict(lengths=[3 + 37 * i % 90 for i in range(1500)] + [3000], new=[i % 3 for i in range(1501)], hq=2, hkv=1, pad_rows=2)], ids=range(5))
+def test_tables_wider_than_the_sequences(case, dtype, d):
+    """Room for 64 thousand tokens each, as a server's table has: the layout of the call follows the room, its work the lengths."""
+    p = Problem(21, dtype=dtype, d=d, **case)
+    wide = torch.full((len(p.lengths), 4096), 10 ** 9, dtype=torch.int32, device=DEV)
+    wide[:, :p.table.shape[1]] = p.dev["page_table"]
+    p.cache = paged.cache_for(p.k, p.v, wide, p.dev["lengths"], p.n_rows, p.dev["cu_new"])
+    p.ws_bytes = B.mmsp_cache_workspace_bytes(p.shape, p.cache)
+    p.ws = torch.full((p.ws_bytes + 256,), 0xff, dtype=torch.uint8, device=DEV)
+    p.check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_groups_of_rows_that_do_not_see_the_same(dtype, value):
+    """40 new tokens of 7 heads a KV head, 280 rows in 9 groups: those before the odd token are as without it, bit for bit."""
+    p = Problem(22, [70, 700], [40, 40], dtype=dtype, hq=14, hkv=2, page=32)
+    clean = p.run()
+    for s, n in enumerate((70, 700)):
+        token = n - 40 + 23
+        page, slot = int(p.table[s, token // 32]), token % 32
+        p.k[page, 0, slot, 5] = value
+        p.v[page, :, slot, 1::2] = value
+    odd = p.run()
+    sees = torch.tensor([i % 40 >= 23 for i in range(80)], device=DEV)
+    for a, b in zip(clean, odd):
+        a, b = (a, b) if a.shape[0] == 80 else (a.T, b.T)
+        assert torch.equal(a[~sees], b[~sees])
+    assert not bool(torch.isfinite(odd[1][sees][:, :, 1::2]).any())
+    assert bool(torch.isfinite(odd[1][sees][:, 7:, ::2]).all())
+
+
+def test_more_rows_than_a_grid_has_workgroups():
+    """2^24 rows, of which the last few of each sequence have tokens that exist.  (The rows overlap in memory; they are only read.)"""
+    hkv, d, page = 17, 64, 16
+    new = [(1 << 24) - 1, 4]
+    rows, lengths = sum(new), [5, 3]
+    k, v = (torch.rand((rows + hkv) * d, device=DEV) for _ in range(2))
+    kp, vp = (torch.full((2, hkv, page, d), math.nan, device=DEV) for _ in range(2))
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    cache = paged.cache_for(kp, vp, dev([[1], [0]]), dev(lengths), rows, dev([0, new[0], rows]))
+    shape = B.make_shape(hkv, hkv, d, B.MMSP_F32, 1.0, (d, d), (d, d), 0)
+    B.mmsp_cache_append(shape, cache, None, None, 0, None, k, v)
+    want = [torch.full_like(kp, math.nan) for _ in range(2)]
+    for t, (s, n) in enumerate(zip((1, 0), lengths)):
+        last = (new[0], rows)[t]
+        for j in range(n):
+            at = (last - n + j) * d
+            for w, x in zip(want, (k, v)):
+                w[s, :, j] = x[at:at + hkv * d].view(hkv, d)
+    for got, w in zip((kp, vp), want):
+        assert torch.equal(got.nan_to_num(-1.0), w.nan_to_num(-1.0))
