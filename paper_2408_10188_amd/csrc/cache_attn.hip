@@ -2,7 +2,7 @@
 // share its KV head, so the memory rate bounds it (28/4 heads, one token: 7 of the 16 columns of a matrix instruction, 7 flops a byte).
 //
 // Work.  The (token, head) pairs of a KV head's new rows are one list, as in the forward kernel; groups of kRows of it are
-// stationary.  A pair of (sequence, KV head, group) has the sequence's keys in tiles.  The tiles of all pairs are one sequence that is cut
+// stationary, 16, 32 or 48 of them.  A pair of (sequence, KV head, group) has the sequence's keys in tiles.  The tiles of all pairs are one sequence that is cut
 // into as many equal ranges as there are workgroups, whatever the lengths are: a workgroup goes through the segments
 // of pairs in its range.  A pair inside one range is finished there; at most the first and the last segment of a range are
 // parts of pairs that others share: their (O, maximum, sum) goes to the workspace and a second launch joins them.  The lengths are on the device only,
@@ -29,6 +29,7 @@ namespace {
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
 constexpr int kMaxGroups = 1024;                        // workgroups of a launch
+constexpr int kMaxTeam = 8;                             // .. that read the same keys
 
 struct Partial {
   int32_t* prefix;                                      // [n_seqs + 1] tiles of the sequences before, then the logarithm of a tile's keys
@@ -36,12 +37,21 @@ struct Partial {
   float* o;                                             // [2 W][kRows][d]
 };
 
-// Groups of kRows rows of a KV head's list, and tiles of each of their pairs.
-struct PairShape { int groups, tiles; };
-template <int kRows>
-__device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const SeqRows& r, int tile_bits) {
+// Workgroups come in teams of `size` that read the same keys at the same time for different groups of rows, so that memory is read once and the others find the keys in
+// their L2: blocks b and b + 8 are on the same XCD.  rows: those of a team, size * kRows.
+struct Teams { int count, size; FastDiv rows; };
+struct Place { int team, member; };
+__device__ __forceinline__ Place place_of(const Teams& t, int block) {
+  const int i = block >> 3, q = i / t.size;
+  return {(block & 7) + 8 * q, i - q * t.size};
+}
+__device__ __forceinline__ int block_of(const Teams& t, int team, int member) { return (team & 7) + 8 * ((team >> 3) * t.size + member); }
+
+// Rounds in which a team takes the rows of a KV head's list, and tiles of each of these pairs.
+struct PairShape { int rounds, tiles; };
+__device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const Teams& teams, const SeqRows& r, int tile_bits) {
   PairShape p;
-  p.groups = (int)(((int64_t)r.count * a.group + kRows - 1) / kRows);
+  p.rounds = (int)(((uint32_t)r.count * a.group + teams.rows.d - 1) / teams.rows);
   p.tiles = max(1, (r.length + (1 << tile_bits) - 1) >> tile_bits);   // rows that see nothing have a tile too: someone has to say so
   return p;
 }
@@ -66,11 +76,13 @@ __device__ __forceinline__ void store_row(void* to, int64_t at, const float (&x)
   }
 }
 
-// Asynchronous copy of 64 x 16 bytes to LDS (see dma16), read once and so past the caches: 7.1 TB/s in a large plain read where the default policy
-// reaches 6.2.
-__device__ __forceinline__ void copy_past_caches(const char* base, uint32_t offset, const void* lds_array, int byte_offset) {
+// Asynchronous copy of 64 x 16 bytes to LDS (see dma16).  What is read once goes past the caches: 7.1 TB/s in a large plain read where the default policy reaches
+// 6.2.  What a team shares does not (two members, 16 x 20000 keys: 149 instead of 173 us).
+template <bool kShared>
+__device__ __forceinline__ void copy_piece(const char* base, uint32_t offset, const void* lds_array, int byte_offset) {
   const uint32_t lds = lds_address(lds_array) + (uint32_t)byte_offset;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(lds), "v"(offset), "s"(base) : "memory");
+  if constexpr (kShared) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(lds), "v"(offset), "s"(base) : "memory");
 }
 // Until all but the last n copies have landed; until all LDS reads have returned.
 template <int kN>
@@ -85,7 +97,7 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
 }
 
 // Tiles of a workgroup's range: workgroup w has tiles [w * each, (w + 1) * each) of `total`.  (The host has made sure that there are at most 2^30.)
-__device__ __forceinline__ int tiles_each(int total, int n_groups) { return max(1, (int)(((uint32_t)total + n_groups - 1) / (uint32_t)n_groups)); }
+__device__ __forceinline__ int tiles_each(int total, int n_teams) { return max(1, (int)(((uint32_t)total + n_teams - 1) / (uint32_t)n_teams)); }
 
 // A sum that the host has ruled out comes from a cu_new that is not ascending: no tile is taken.
 __device__ __forceinline__ int checked_total(int total) { return total < 0 || total > 1 << 30 ? 0 : total; }
@@ -97,7 +109,7 @@ __device__ __forceinline__ int checked_total(int total) { return total < 0 || to
 constexpr int kUsualBits = 8;
 constexpr int fewest_bits(bool bf16) { return bf16 ? 7 : 6; }
 template <int kFewest, class Tiles>
-__device__ __forceinline__ int pick_tile(Tiles tiles, int n_groups) {
+__device__ __forceinline__ int pick_tile(Tiles tiles, int n_teams) {
   constexpr int kMost = 9;
   int n[kMost - kFewest + 1];
 #pragma unroll
@@ -108,12 +120,12 @@ __device__ __forceinline__ int pick_tile(Tiles tiles, int n_groups) {
     for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] += __shfl_xor(n[b - kFewest], w);
   int bits = kUsualBits;
 #pragma unroll
-  for (int b = kMost; b >= kFewest; --b) bits = n[b - kFewest] <= n_groups ? b : bits;
+  for (int b = kMost; b >= kFewest; --b) bits = n[b - kFewest] <= n_teams ? b : bits;
   return __builtin_amdgcn_readfirstlane(bits);
 }
 
 template <bool kBf16, int kD, int kNT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArgs a, int n_groups, int tile_bits, Partial part) {
+__global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArgs a, Teams teams, int tile_bits, Partial part) {
   constexpr int kThreads = 64 * kWaves;
   constexpr int kRows = 16 * kNT, kElt = kBf16 ? 2 : 4;
   constexpr int kBlocks = kBf16 ? 2 : 1, kKeys = 16 * kBlocks;   // blocks of 16 keys, keys of a step
@@ -126,6 +138,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
   __shared__ __attribute__((aligned(1024))) char ring[kWaves * 2 * kHalf];
   static_assert(kWaves * 16 * kPad * 4 <= (int)sizeof(ring), "the results of a tile of rows fit");
   float (*const red)[16][kPad] = reinterpret_cast<float (*)[16][kPad]>(ring);
+  // Q of 48 rows is read from LDS for each step, as K is: in registers it would leave too few for two workgroups a CU.
+  constexpr bool kSharedQ = kNT > 2;
+  __shared__ __attribute__((aligned(16))) char q_rows[kSharedQ ? kRows * kD * kElt : 16];
   __shared__ float red_m[kWaves][kRows], red_l[kWaves][kRows];
   __shared__ int wave_tiles[kWaves], found[2];
 
@@ -133,18 +148,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
   const int col = lane & 15, quad = lane >> 4;
   const CacheArgs& c = a.cache;
 
-  // ---- this workgroup's range of tiles ----
+  // ---- this team's range of tiles ----
+  const Place me = place_of(teams, blockIdx.x);
   // (Every bound below also holds where cu_new is not ascending and the sums are nonsense.)
   auto tiles_of = [&](const SeqRows& r, int bits) {
-    const PairShape p = pairs_of<kRows>(a, r, bits);
-    return p.groups * a.Hkv * p.tiles;
+    const PairShape p = pairs_of(a, teams, r, bits);
+    return p.rounds * a.Hkv * p.tiles;
   };
   const bool few = c.n_seqs <= 64;                      // every wavefront has all sequences in its lanes: no LDS, no second look at memory
   SeqRows mine = {};                                    // of sequence `lane`, if few
   int t, t_end, seq, base;                              // the next tile, the range's end; the tile's sequence, and tiles before that one
   if (few) {
     if (lane < c.n_seqs) mine = rows_of_seq(c, lane);
-    if (tile_bits < 0) tile_bits = pick_tile<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, n_groups);
+    if (tile_bits < 0) tile_bits = pick_tile<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, teams.count);
     const int n = lane < c.n_seqs ? tiles_of(mine, tile_bits) : 0;
     int upto = n;
 #pragma unroll
@@ -157,8 +173,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       if (lane < c.n_seqs) part.prefix[lane] = upto - n;
       if (lane == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
     }
-    const int each = tiles_each(total, n_groups);
-    t = blockIdx.x * each;
+    const int each = tiles_each(total, teams.count);
+    t = me.team * each;
     t_end = min(t + each, total);
     if (t >= t_end) return;
     seq = 63 - __builtin_clzll(__ballot(lane < c.n_seqs && upto - n <= t) | 1);   // the last one that begins by then
@@ -189,8 +205,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       for (int s = s_first; s < s_last; ++s) { part.prefix[s] = x; x += tiles_of(rows_of_seq(c, s), tile_bits); }
       if (tid == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
     }
-    const int each = tiles_each(total, n_groups);
-    t = blockIdx.x * each;
+    const int each = tiles_each(total, teams.count);
+    t = me.team * each;
     t_end = min(t + each, total);
     if (t >= t_end) return;
     if (upto - n <= t && t < upto) {                    // one thread
@@ -226,28 +242,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       r.count = __builtin_amdgcn_readfirstlane(r.count);
       r.length = __builtin_amdgcn_readfirstlane(r.length);
     }
-    const PairShape shape = pairs_of<kRows>(a, r, tile_bits);
-    const int n_seq = shape.groups * a.Hkv * shape.tiles;
+    const PairShape shape = pairs_of(a, teams, r, tile_bits);
+    const int n_seq = shape.rounds * a.Hkv * shape.tiles;
     if (t >= base + n_seq) { base += n_seq; ++seq; continue; }
     const int pair = (int)((uint32_t)(t - base) / (uint32_t)shape.tiles);
     const int tile0 = __builtin_amdgcn_readfirstlane(t - base - pair * shape.tiles);
     const int tile1 = __builtin_amdgcn_readfirstlane(min(shape.tiles, tile0 + (t_end - t)));
-    const int kvh = __builtin_amdgcn_readfirstlane((int)((uint32_t)pair / (uint32_t)shape.groups)), group0 = __builtin_amdgcn_readfirstlane((pair - kvh * shape.groups) * kRows);
+    const int kvh = __builtin_amdgcn_readfirstlane((int)((uint32_t)pair / (uint32_t)shape.rounds));
+    const int group0 = __builtin_amdgcn_readfirstlane(((pair - kvh * shape.rounds) * teams.size + me.member) * kRows);
     t += tile1 - tile0;
 
     // ---- rows ----
     const int n_list = r.count * a.group, first_pos = r.length - r.count;
+    if (group0 >= n_list) continue;                     // fewer groups than the team has members
     int hi[kNT];                                        // last key that this lane's rows see
-    u32x4 q[kNT][kKL];
+    u32x4 q[kSharedQ ? 1 : kNT][kKL];
 #pragma unroll
     for (int j = 0; j < kNT; ++j) {
       const int i = group0 + j * 16 + col, ic = min(i, n_list - 1);
       const int tok = (int)((uint32_t)ic / a.group_div);
       hi[j] = first_pos + tok;                          // a row behind the last one does as that one
       const char* p = reinterpret_cast<const char*>(a.q) + ((int64_t)(r.first + tok) * a.q_ts + (kvh * a.group + ic - tok * a.group) * a.q_hs) * kElt + quad * 16;
+      if (kSharedQ && wave != j) continue;
 #pragma unroll
-      for (int i2 = 0; i2 < kKL; ++i2) q[j][i2] = *reinterpret_cast<const u32x4*>(p + i2 * 64);
+      for (int i2 = 0; i2 < kKL; ++i2) q[kSharedQ ? 0 : j][i2] = *reinterpret_cast<const u32x4*>(p + i2 * 64);
+      if constexpr (kSharedQ)
+#pragma unroll
+        for (int i2 = 0; i2 < kKL; ++i2) *reinterpret_cast<u32x4*>(q_rows + (j * 16 + col) * kD * kElt + ((i2 * 4 + quad) ^ col) * 16) = q[0][i2];
     }
+    static_assert(!kSharedQ || (kNT <= kWaves && kD * kElt == 256), "a wavefront for each 16 rows of Q, 16 pieces a row");
+    if constexpr (kSharedQ) __syncthreads();
     const int hi_max = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)(min(group0 + kRows, n_list) - 1) / a.group_div));
     const int hi_min = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)group0 / a.group_div));
     const int key_end = __builtin_amdgcn_readfirstlane(min((int)min((int64_t)tile1 << tile_bits, (int64_t)INT32_MAX), hi_max + 1));
@@ -313,19 +337,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       }
       return true;
     };
-    auto copy_k = [&](const Step& x) {
+    const bool team = kNT > 1 && teams.size > 1;
+    auto k_copies = [&](auto shared, const Step& x) {
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < kBlockCopies; ++i) copy_past_caches(k_head + x.at[b], k_lane[i], ring, wave * 2 * kHalf + (b * kBlockCopies + i) * 1024);
+        for (int i = 0; i < kBlockCopies; ++i) copy_piece<shared>(k_head + x.at[b], k_lane[i], ring, wave * 2 * kHalf + (b * kBlockCopies + i) * 1024);
     };
-    auto copy_v = [&](const Step& x) {
+    auto v_copies = [&](auto shared, const Step& x) {
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int i = 0; i < kBlockCopies; ++i)
-          copy_past_caches(v_head + x.at[b] + (int64_t)i * (64 / kRowChunks) * row_bytes, v_lane, ring, wave * 2 * kHalf + kHalf + (b * kBlockCopies + i) * 1024);
+          copy_piece<shared>(v_head + x.at[b] + (int64_t)i * (64 / kRowChunks) * row_bytes, v_lane, ring, wave * 2 * kHalf + kHalf + (b * kBlockCopies + i) * 1024);
     };
+    auto copy_k = [&](const Step& x) { if (team) k_copies(std::true_type(), x); else k_copies(std::false_type(), x); };
+    auto copy_v = [&](const Step& x) { if (team) v_copies(std::true_type(), x); else v_copies(std::false_type(), x); };
     // The step's copies are on their way, K's before V's; the following step's K is asked for as soon as this
     // one's has been read, and so is V.
     auto compute = [&](const Step& x, bool more, const Step& after) {
@@ -346,16 +373,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       f32x4 p[kNT][kBlocks];
 #pragma unroll
       for (int j = 0; j < kNT; ++j) {
+        u32x4 qj[kKL];
+#pragma unroll
+        for (int i = 0; i < kKL; ++i) {
+          if constexpr (kSharedQ) qj[i] = *reinterpret_cast<const u32x4*>(q_rows + (j * 16 + col) * kD * kElt + ((i * 4 + quad) ^ col) * 16);
+          else qj[i] = q[j][i];
+        }
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
           f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < kKL; ++i) {
             if constexpr (kBf16) {
-              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[b][i]), __builtin_bit_cast(bf16x8, q[j][i]), s, 0, 0, 0);
+              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[b][i]), __builtin_bit_cast(bf16x8, qj[i]), s, 0, 0, 0);
             } else {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[b][i][e]), __uint_as_float(q[j][i][e]), s, 0, 0, 0);
+              for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[b][i][e]), __uint_as_float(qj[i][e]), s, 0, 0, 0);
             }
           }
           if (!whole) {
@@ -484,10 +517,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
     if (key_of(0) < key_end) refill();
     // Q has landed too, since it was asked for before the pages.  Left to the compiler the wait for it would stand in the loop, where the same counter
     // holds the copies.
+    if constexpr (!kSharedQ)
 #pragma unroll
-    for (int j = 0; j < kNT; ++j)
+      for (int j = 0; j < kNT; ++j)
 #pragma unroll
-      for (int i = 0; i < kKL; ++i) asm volatile("" : "+v"(q[j][i]));
+        for (int i = 0; i < kKL; ++i) asm volatile("" : "+v"(q[j][i]));
     bool have = next(now);
     if (have) {
       copy_k(now);
@@ -583,7 +617,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
 // of them needs is asked for at once: 28 workgroups that join 128 partial results each took
 // 10.8 us with maxima, sums and results after one another, and take 6.1 (64 partial results: 4.9).
 template <bool kBf16, int kD, int kRows>
-__global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, int n_groups, Partial part) {
+__global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, Teams teams, Partial part) {
   constexpr int kTeam = kD / 4, kTeams = 256 / kTeam, kBatch = 4;
   __shared__ f32x4 xs[kTeams][kTeam];
   __shared__ float ls[kTeams], tops[4], ms[kMaxGroups], sums[kMaxGroups];
@@ -609,12 +643,13 @@ __global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, int
   if (row < r.first || row - r.first >= r.count) return;
   const int kvh = (int)((uint32_t)h / a.group_div), i = (row - r.first) * a.group + h - kvh * a.group, jr = i % kRows;
   const int tile_bits = part.prefix[c.n_seqs + 1];
-  const PairShape shape = pairs_of<kRows>(a, r, tile_bits);
-  const int t0 = part.prefix[seq] + (kvh * shape.groups + i / kRows) * shape.tiles, each = tiles_each(part.prefix[c.n_seqs], n_groups);
+  const PairShape shape = pairs_of(a, teams, r, tile_bits);
+  const int round = (int)((uint32_t)i / teams.rows), member = i / kRows - round * teams.size;
+  const int t0 = part.prefix[seq] + (kvh * shape.rounds + round) * shape.tiles, each = tiles_each(part.prefix[c.n_seqs], teams.count);
   const int w0 = (int)((uint32_t)t0 / (uint32_t)each), count = (int)((uint32_t)(t0 + shape.tiles - 1) / (uint32_t)each) - w0 + 1;
-  if (count <= 1 || t0 < 0 || w0 >= n_groups || count > n_groups - w0) return;   // finished where it was computed (or cu_new is not ascending)
+  if (count <= 1 || t0 < 0 || w0 >= teams.count || count > teams.count - w0) return;   // finished where it was computed (or cu_new is not ascending)
   const int team = tid / kTeam, e = tid % kTeam;
-  auto at = [&](int s) { return (2 * (int64_t)(w0 + s) + (s == 0 ? 1 : 0)) * kRows + jr; };
+  auto at = [&](int s) { return (2 * (int64_t)block_of(teams, w0 + s, member) + (s == 0 ? 1 : 0)) * kRows + jr; };
   f32x4 y[kBatch];
   auto ask = [&](int first) {
 #pragma unroll
@@ -672,19 +707,28 @@ __global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, int
   if (a.lse != nullptr && e == 0) a.lse[h * a.lse_hs + row] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// How a call is laid out: tiles of 16 rows of a workgroup's group, wavefronts of a workgroup, workgroups, the logarithm of a tile's keys (-1: picked by the
+// How a call is laid out: tiles of 16 rows of a workgroup's group, wavefronts of a workgroup, teams and their members, the logarithm of a tile's keys (-1: picked by the
 // kernel), and whether several workgroups may share a pair.
-struct Plan { int nt, waves, groups, tile_bits; bool shared; double most; };   // most: tiles of all pairs at most
+struct Plan { int nt, waves, team_size, teams, tile_bits; bool shared; double most; };   // most: tiles of all pairs at most
 Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   const CacheArgs& c = a.cache;
   const int n_cu = cu_count();
-  // The rows of a sequence in one group where 32 hold them: every further group reads the keys again.  With ragged numbers of new tokens, twice the mean.
-  // (Groups of 48 rows, one workgroup a CU: 28/4 heads, 5 new tokens on 65536: 37.8 instead of 43.7 us, 16 new ones 82.3 instead of 61.2.)
-  const int64_t rows_each = c.cu_new == nullptr ? a.group : 2 * ((int64_t)c.n_rows * a.group / c.n_seqs);
+  // Rows of a sequence: the same number each if that can be, or else twice the mean.
+  const int64_t rows_all = (int64_t)c.n_rows * a.group, rows_each = std::max<int64_t>(1, (c.n_rows % c.n_seqs == 0 ? 1 : 2) * (rows_all / c.n_seqs));
+  // Groups of 32 rows, or of 48 (bf16) where they need fewer workgroups, in teams of a power of two (three members do not find each other's keys).  28/4 heads, 16
+  // sequences of 20000 keys, us with groups of 48 / of 32: 5 new tokens 122 / 144, 9 148 / 150, 13 167 / 222, 16 257 / 228, 20 261 / 352, 32 467 / 364; without teams 9
+  // took 222, 16 342.
+  auto workgroups = [&](int nt) {
+    const int64_t groups = (rows_each + 16 * nt - 1) / (16 * nt);
+    int64_t n = 1;
+    while (n < kMaxTeam && n < groups) n *= 2;
+    return (groups + n - 1) / n * n;
+  };
   Plan p;
-  p.nt = rows_each <= 16 ? 1 : 2;
+  p.nt = rows_each <= 16 ? 1 : bf16 && workgroups(3) < workgroups(2) ? 3 : 2;
+  p.team_size = (int)std::min<int64_t>(kMaxTeam, workgroups(p.nt));
   const int64_t capacity = (int64_t)c.max_pages * c.page_size;
-  const double pairs = (double)((int64_t)c.n_rows * a.group / (16 * p.nt) + c.n_seqs) * a.Hkv;
+  const double pairs = (double)(rows_all / (16 * p.nt * p.team_size) + c.n_seqs) * a.Hkv;
   // A short cache: one workgroup for a pair, and no second launch.  28/4 heads, us so and with shared pairs: 8 sequences of 400 tokens 9.5 and 11.4, of
   // 900 14.1 and 11.7; 60 of 900 21.4 and 27.7, 200 of 900 64.5 and 75.7, of 20 to 900 39.0 and 37.9, of 1900 138.0 and 138.9.
   p.shared = capacity > (pairs * 2 >= n_cu ? 1024 : 512) / (bf16 ? 1 : 2);
@@ -695,7 +739,8 @@ Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   p.tile_bits = p.shared ? -1 : 30;
   const int fewest = 1 << fewest_bits(bf16);
   p.most = pairs * (p.shared ? (double)((capacity + fewest - 1) / fewest) : 1.);
-  p.groups = (int)std::min<double>(std::min(kMaxGroups, n_cu * (p.waves == 4 ? 2 : 1)), p.most);
+  p.teams = (int)std::min<double>(std::min(kMaxGroups, n_cu * (p.waves == 4 ? 2 : 1)) / p.team_size, p.most);
+  if (p.team_size > 1) p.teams = (p.teams + 7) / 8 * 8;  // all blocks of a team exist
   return p;
 }
 
@@ -707,7 +752,7 @@ double cache_attn_tiles(const CacheAttnArgs& a, int io_dtype) { return plan_of(a
 
 int64_t cache_attn_workspace_bytes(const CacheAttnArgs& a, int io_dtype) {
   const Plan p = plan_of(a, io_dtype == 0);
-  return align16(4 * ((int64_t)a.cache.n_seqs + 2)) + (int64_t)2 * p.groups * 16 * p.nt * 4 * (2 + a.d);
+  return align16(4 * ((int64_t)a.cache.n_seqs + 2)) + (int64_t)2 * p.teams * p.team_size * 16 * p.nt * 4 * (2 + a.d);
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t stream) {
@@ -717,21 +762,24 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t s
   char* w = a.ws;
   part.prefix = reinterpret_cast<int32_t*>(w);
   w += align16(4 * ((int64_t)a.cache.n_seqs + 2));
-  const int64_t rows = (int64_t)2 * p.groups * 16 * p.nt;
+  const int64_t rows = (int64_t)2 * p.teams * p.team_size * 16 * p.nt;
+  const Teams teams = {p.teams, p.team_size, fast_div(16 * p.nt * p.team_size)};
   part.o = reinterpret_cast<float*>(w);
   part.m = part.o + rows * a.d;
   part.l = part.m + rows;
   auto launch = [&](auto bf16, auto d, auto nt, auto waves) {
     constexpr bool kBf16 = decltype(bf16)::value;
     constexpr int kD = decltype(d)::value, kNT = decltype(nt)::value, kWaves = decltype(waves)::value;
-    cache_attn_kernel<kBf16, kD, kNT, kWaves><<<dim3((unsigned)p.groups), dim3(64 * kWaves), 0, stream>>>(a, p.groups, p.tile_bits, part);
+    cache_attn_kernel<kBf16, kD, kNT, kWaves><<<dim3((unsigned)(p.teams * p.team_size)), dim3(64 * kWaves), 0, stream>>>(a, teams, p.tile_bits, part);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !p.shared || p.groups == 1) return e;
-    cache_join_kernel<kBf16, kD, 16 * kNT><<<dim3((unsigned)((int64_t)a.cache.n_rows * a.Hq)), dim3(256), 0, stream>>>(a, p.groups, part);
+    if (e != hipSuccess || !p.shared || p.teams == 1) return e;
+    cache_join_kernel<kBf16, kD, 16 * kNT><<<dim3((unsigned)((int64_t)a.cache.n_rows * a.Hq)), dim3(256), 0, stream>>>(a, teams, part);
     return hipGetLastError();
   };
   auto by_rows = [&](auto bf16, auto d) {
     using four = std::integral_constant<int, 4>;
+    if constexpr (decltype(bf16)::value)
+      if (p.nt == 3) return launch(bf16, d, std::integral_constant<int, 3>(), four());
     if (p.nt == 2) return launch(bf16, d, std::integral_constant<int, 2>(), four());
     if (p.waves == 4) return launch(bf16, d, std::integral_constant<int, 1>(), four());
     return launch(bf16, d, std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
