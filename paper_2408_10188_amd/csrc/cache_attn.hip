@@ -109,13 +109,13 @@ __device__ __forceinline__ int checked_total(int total) { return total < 0 || to
 constexpr int kUsualBits = 8;
 constexpr int fewest_bits(bool bf16) { return bf16 ? 7 : 6; }
 template <int kFewest, class Tiles>
-__device__ __forceinline__ int pick_tile(Tiles tiles, int n_teams) {
+__device__ __forceinline__ int pick_tile(Tiles tiles, int n_seqs, int n_teams) {
   constexpr int kMost = 9;
   int n[kMost - kFewest + 1];
 #pragma unroll
   for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] = min(tiles(b), 1 << 24);   // 64 of them stay below 2^31
-#pragma unroll
-  for (int w = 1; w < 64; w <<= 1)
+#pragma unroll 1
+  for (int w = 1; w < n_seqs; w <<= 1)
 #pragma unroll
     for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] += __shfl_xor(n[b - kFewest], w);
   int bits = kUsualBits;
@@ -132,12 +132,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
   constexpr int kKL = kD * kElt / 64;                   // 16-byte pieces of a K row that a lane holds
   constexpr int kVC = kD * kElt / 256;                  // .. of a V row
   constexpr int kAcc = kD / 16;                         // O^T accumulators of 16 rows of d
-  constexpr int kPad = kD + 4;
   constexpr int kHalf = kKeys * kD * kElt, kCopies = kHalf / 1024;   // bytes of a step's K (or V), copies that bring them
-  // A wavefront's K and V of a step; when a segment ends, the wavefronts' O, [kWaves][16][kPad] floats.
+  // A wavefront's K and V of a step; when a segment ends, the wavefronts' O for kAtOnce tiles of 16 rows, [kAtOnce][kWaves][16][kD] floats, each row's pieces of 4 in
+  // places piece ^ row.
   __shared__ __attribute__((aligned(1024))) char ring[kWaves * 2 * kHalf];
-  static_assert(kWaves * 16 * kPad * 4 <= (int)sizeof(ring), "the results of a tile of rows fit");
-  float (*const red)[16][kPad] = reinterpret_cast<float (*)[16][kPad]>(ring);
+  constexpr int kTileFloats = kWaves * 16 * kD, kAtOnce = (int)sizeof(ring) / (4 * kTileFloats) < kNT ? (int)sizeof(ring) / (4 * kTileFloats) : kNT;
+  static_assert(kAtOnce >= 1, "the results of a tile of rows fit");
+  float* const red = reinterpret_cast<float*>(ring);
+  auto red_at = [&](int tile, int w, int row, int d) { return red + (tile * kTileFloats + (w * 16 + row) * kD + ((d >> 2 ^ row) << 2) + (d & 3)); };
   // Q of 48 rows is read from LDS for each step, as K is: in registers it would leave too few for two workgroups a CU.
   constexpr bool kSharedQ = kNT > 2;
   __shared__ __attribute__((aligned(16))) char q_rows[kSharedQ ? kRows * kD * kElt : 16];
@@ -160,15 +162,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
   int t, t_end, seq, base;                              // the next tile, the range's end; the tile's sequence, and tiles before that one
   if (few) {
     if (lane < c.n_seqs) mine = rows_of_seq(c, lane);
-    if (tile_bits < 0) tile_bits = pick_tile<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, teams.count);
+    if (tile_bits < 0) tile_bits = pick_tile<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, c.n_seqs, teams.count);
     const int n = lane < c.n_seqs ? tiles_of(mine, tile_bits) : 0;
     int upto = n;
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) {
+#pragma unroll 1
+    for (int w = 1; w < c.n_seqs; w <<= 1) {
       const int x = __shfl_up(upto, w);
       if (lane >= w) upto += x;
     }
-    const int total = checked_total(__builtin_amdgcn_readlane(upto, 63));
+    const int total = checked_total(__builtin_amdgcn_readlane(upto, c.n_seqs - 1));
     if (blockIdx.x == 0 && wave == 0) {                 // for the joining launch
       if (lane < c.n_seqs) part.prefix[lane] = upto - n;
       if (lane == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
@@ -452,8 +454,33 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
             if (!(x.here >> b & 1) || x.k0 + 16 * b + quad * 4 + r > hi_max)
 #pragma unroll
               for (int e = 0; e < kVC; ++e) *reinterpret_cast<u32x4*>(v_mine + (b * 16 + r) * kD * kElt + e * 256) = mk4(0u, 0u, 0u, 0u);
-        // Nor is an infinity or NaN that some rows see and others do not: it is left out here and added to the rows that see it after the loop.
-        if (hi_min < hi_max && x.k0 + kKeys - 1 > hi_min) {
+      }
+      u32x4 v[kBlocks][4][kVC];
+      auto read_v = [&] {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < kVC; ++e) v[b][r][e] = *reinterpret_cast<const u32x4*>(v_mine + (b * 16 + r) * kD * kElt + e * 256);
+      };
+      read_v();
+      // Nor is an infinity or NaN that some rows see and others do not: it is left out here and added to the rows that see it after the loop.
+      if (!whole && hi_min < hi_max && x.k0 + kKeys - 1 > hi_min) {
+        constexpr uint32_t kOne = kBf16 ? 0x00800080u : 0x00800000u, kExponents = kBf16 ? 0x7f807f80u : 0x7f800000u, kCarries = kBf16 ? 0x80008000u : 0x80000000u;
+        uint32_t carry = 0;                              // exponents of ones only, and one more
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            uint32_t of_key = 0;
+#pragma unroll
+            for (int e = 0; e < kVC; ++e)
+#pragma unroll
+              for (int w = 0; w < 4; ++w) of_key |= (v[b][r][e][w] & kExponents) + kOne;
+            carry |= x.k0 + 16 * b + quad * 4 + r > hi_min ? of_key : 0u;
+          }
+        if (__any((carry & kCarries) != 0)) {
 #pragma unroll 1
           for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -474,15 +501,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
                   odd = true;
                 }
               }
+          read_v();
         }
       }
-      u32x4 v[kBlocks][4][kVC];
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int e = 0; e < kVC; ++e) v[b][r][e] = *reinterpret_cast<const u32x4*>(v_mine + (b * 16 + r) * kD * kElt + e * 256);
       if (more) {
         wait_reads();
         copy_v(after);
@@ -565,46 +586,57 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
     const bool finished = tile0 == 0 && tile1 == shape.tiles;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (tile0 == 0 ? 1 : 0);
 #pragma unroll
-    for (int j = 0; j < kNT; ++j) {
+    for (int j0 = 0; j0 < kNT; j0 += kAtOnce) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int j = j0; j < min(j0 + kAtOnce, kNT); ++j)
 #pragma unroll
-        for (int e = 0; e < kAcc; e += 4) {
-          // bf16: accumulators 0..7 are 8 consecutive d; f32: 0..3 (4..7 of the upper half) are 4
-          const int d = kBf16 ? (quad * 4 + i) * 8 + e : (e / 4) * 64 + (quad * 4 + i) * 4;
-          *reinterpret_cast<f32x4*>(&red[wave][col][d]) = f32x4{acc[j][e][i], acc[j][e + 1][i], acc[j][e + 2][i], acc[j][e + 3][i]};
-        }
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < kAcc; e += 4) {
+            // bf16: accumulators 0..7 are 8 consecutive d; f32: 0..3 (4..7 of the upper half) are 4
+            const int d = kBf16 ? (quad * 4 + i) * 8 + e : (e / 4) * 64 + (quad * 4 + i) * 4;
+            *reinterpret_cast<f32x4*>(red_at(j - j0, wave, col, d)) = f32x4{acc[j][e][i], acc[j][e + 1][i], acc[j][e + 2][i], acc[j][e + 3][i]};
+          }
       __syncthreads();
-      constexpr int kShare = kThreads / 16, kEach = kD / kShare;   // threads of a row, elements of each
-      const int row = tid / kShare, jr = j * 16 + row, d0 = tid % kShare * kEach;
-      float top = red_m[0][jr];
+      constexpr int kShare = kThreads / 16, kEach = kD / kShare, kPiece = kEach < 4 ? kEach : 4;   // threads of a row, elements of each, .. at once
+      typedef __attribute__((__vector_size__(kPiece * sizeof(float)))) float piece_t;
+      const int row = tid / kShare, d0 = tid % kShare * kEach;
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w][jr]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, x[kEach];
+      for (int j = j0; j < min(j0 + kAtOnce, kNT); ++j) {
+        const int jr = j * 16 + row;
+        float top = red_m[0][jr];
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) x[e] = 0.f;
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w][jr]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float sum = 0.f, x[kEach];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(red_m[w][jr] - ref);
-        sum += f * red_l[w][jr];
+        for (int e = 0; e < kEach; ++e) x[e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) x[e] += f * red[w][row][d0 + e];
-      }
-      const int i = group0 + jr;
-      if (i < n_list) {
-        if (finished) {
-          const int tok = (int)((uint32_t)i / a.group_div), h = kvh * a.group + i - tok * a.group;
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          const int64_t at = ((int64_t)(r.first + tok) * a.Hq + h) * kD + d0;
+        for (int w = 0; w < kWaves; ++w) {
+          const float f = __builtin_amdgcn_exp2f(red_m[w][jr] - ref);
+          sum += f * red_l[w][jr];
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) x[e] *= inv;
-          if (a.o != nullptr) store_row<false>(a.o, at, x);
-          if (a.o_final != nullptr) store_row<kBf16>(a.o_final, at, x);
-          if (a.lse != nullptr && d0 == 0) a.lse[h * a.lse_hs + r.first + tok] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
-        } else {
-          store_row<false>(part.o, (slot * kRows + jr) * kD + d0, x);
-          if (d0 == 0) { part.m[slot * kRows + jr] = top; part.l[slot * kRows + jr] = sum; }
+          for (int e = 0; e < kEach; e += kPiece) {
+            const piece_t y = *reinterpret_cast<const piece_t*>(red_at(j - j0, w, row, d0 + e));
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k) x[e + k] += f * y[k];
+          }
+        }
+        const int i = group0 + jr;
+        if (i < n_list) {
+          if (finished) {
+            const int tok = (int)((uint32_t)i / a.group_div), h = kvh * a.group + i - tok * a.group;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const int64_t at = ((int64_t)(r.first + tok) * a.Hq + h) * kD + d0;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) x[e] *= inv;
+            if (a.o != nullptr) store_row<false>(a.o, at, x);
+            if (a.o_final != nullptr) store_row<kBf16>(a.o_final, at, x);
+            if (a.lse != nullptr && d0 == 0) a.lse[h * a.lse_hs + r.first + tok] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+          } else {
+            store_row<false>(part.o, (slot * kRows + jr) * kD + d0, x);
+            if (d0 == 0) { part.m[slot * kRows + jr] = top; part.l[slot * kRows + jr] = sum; }
+          }
         }
       }
       __syncthreads();
