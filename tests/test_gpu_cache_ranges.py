@@ -67,3 +67,14 @@ def test_more_rows_than_a_grid_has_workgroups():
                 w[s, :, j] = x[at:at + hkv * d].view(hkv, d)
     for got, w in zip((kp, vp), want):
         assert torch.equal(got.nan_to_num(-1.0), w.nan_to_num(-1.0))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [[2], [4, 4], [5, 5], [6], [7, 7], [13], [14, 14], [20], [21], [28, 28], [54], [55], [110], [1, 20, 0, 6], [0, 0, 9], [40, 1, 1, 1, 1]],
+                         ids=lambda x: "-".join(map(str, x)))
+def test_numbers_of_rows_around_the_layouts(new, dtype):
+    """Seven heads a KV head: 14 to 770 rows, one group, teams of two, four and eight, full and not, and more groups than a team takes at once; with the
+    same number of new tokens in every sequence and with ragged ones."""
+    lengths = [n + 100 + 517 * (i % 3) for i, n in enumerate(new)]
+    Problem(23, lengths, new, dtype=dtype, hq=14, hkv=2, page=16, pad_rows=len(new) % 2).check()
+    Problem(24, [n + 3000 for n in new], new, dtype=dtype, hq=7, hkv=1, page=64).check()
