@@ -32,7 +32,7 @@ constexpr int kMaxGroups = 1024;                        // workgroups of a launc
 constexpr int kMaxTeam = 8;                             // .. that read the same keys
 
 struct Partial {
-  int32_t* prefix;                                      // [n_seqs + 1] tiles of the sequences before, then the logarithm of a tile's keys
+  u32x2* parts;                                         // [n_rows][Hq] the block that has the first tile, and (how many teams have some) << 8 | row of its group
   float* m; float* l;                                   // [2 W][kRows]
   float* o;                                             // [2 W][kRows][d]
 };
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
   };
   const bool few = c.n_seqs <= 64;                      // every wavefront has all sequences in its lanes: no LDS, no second look at memory
   SeqRows mine = {};                                    // of sequence `lane`, if few
-  int t, t_end, seq, base;                              // the next tile, the range's end; the tile's sequence, and tiles before that one
+  int each, t, t_end, seq, base;                        // tiles of a range, the next tile, the range's end; the tile's sequence, and tiles before that one
   if (few) {
     if (lane < c.n_seqs) mine = rows_of_seq(c, lane);
     if (tile_bits < 0) tile_bits = pick_tile<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, c.n_seqs, teams.count);
@@ -171,11 +171,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       if (lane >= w) upto += x;
     }
     const int total = checked_total(__builtin_amdgcn_readlane(upto, c.n_seqs - 1));
-    if (blockIdx.x == 0 && wave == 0) {                 // for the joining launch
-      if (lane < c.n_seqs) part.prefix[lane] = upto - n;
-      if (lane == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
-    }
-    const int each = tiles_each(total, teams.count);
+    each = tiles_each(total, teams.count);
     t = me.team * each;
     t_end = min(t + each, total);
     if (t >= t_end) return;
@@ -202,12 +198,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       total += wave_tiles[w];
     }
     total = checked_total(__builtin_amdgcn_readfirstlane(total));
-    if (blockIdx.x == 0) {
-      int x = upto - n;
-      for (int s = s_first; s < s_last; ++s) { part.prefix[s] = x; x += tiles_of(rows_of_seq(c, s), tile_bits); }
-      if (tid == 0) { part.prefix[c.n_seqs] = total; part.prefix[c.n_seqs + 1] = tile_bits; }
-    }
-    const int each = tiles_each(total, teams.count);
+    each = tiles_each(total, teams.count);
     t = me.team * each;
     t_end = min(t + each, total);
     if (t >= t_end) return;
@@ -252,6 +243,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
     const int tile1 = __builtin_amdgcn_readfirstlane(min(shape.tiles, tile0 + (t_end - t)));
     const int kvh = __builtin_amdgcn_readfirstlane((int)((uint32_t)pair / (uint32_t)shape.rounds));
     const int group0 = __builtin_amdgcn_readfirstlane(((pair - kvh * shape.rounds) * teams.size + me.member) * kRows);
+    // teams that have tiles of this pair, from the one with its first tile on
+    const int n_parts = __builtin_amdgcn_readfirstlane((int)((uint32_t)(t - tile0 + shape.tiles - 1) / (uint32_t)each) - me.team + 1);
     t += tile1 - tile0;
 
     // ---- rows ----
@@ -624,10 +617,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
         }
         const int i = group0 + jr;
         if (i < n_list) {
+          const int tok = (int)((uint32_t)i / a.group_div), h = kvh * a.group + i - tok * a.group;
+          const int64_t row_head = (int64_t)(r.first + tok) * a.Hq + h;
+          if (tile0 == 0 && d0 == 0) part.parts[row_head] = u32x2{blockIdx.x, (uint32_t)n_parts << 8 | (uint32_t)jr};
           if (finished) {
-            const int tok = (int)((uint32_t)i / a.group_div), h = kvh * a.group + i - tok * a.group;
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const int64_t at = ((int64_t)(r.first + tok) * a.Hq + h) * kD + d0;
+            const int64_t at = row_head * kD + d0;
 #pragma unroll
             for (int e = 0; e < kEach; ++e) x[e] *= inv;
             if (a.o != nullptr) store_row<false>(a.o, at, x);
@@ -645,7 +640,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
 }
 
 // Joins the partial results of pairs that several workgroups shared.  A workgroup takes one (row, head); teams of d / 4 threads share out the partial
-// results.  It is a chain of latencies: which sequence and which partial results, these with their maxima and sums, the result.  All that one
+// results.  It is a chain of latencies: which partial results, these with their maxima and sums, the result.  All that one
 // of them needs is asked for at once: 28 workgroups that join 128 partial results each took
 // 10.8 us with maxima, sums and results after one another, and take 6.1 (64 partial results: 4.9).
 template <bool kBf16, int kD, int kRows>
@@ -653,40 +648,23 @@ __global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, Tea
   constexpr int kTeam = kD / 4, kTeams = 256 / kTeam, kBatch = 4;
   __shared__ f32x4 xs[kTeams][kTeam];
   __shared__ float ls[kTeams], tops[4], ms[kMaxGroups], sums[kMaxGroups];
-  __shared__ int before[4];
   const CacheArgs& c = a.cache;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.x / a.Hq, h = blockIdx.x - row * a.Hq;
-  int seq = row;
-  if (c.cu_new != nullptr && c.n_seqs <= 1024) {        // counted, not searched for: one latency
-    int n = 0;
-    for (int s = tid; s < c.n_seqs; s += 256) n += c.cu_new[s + 1] <= row;
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) n += __shfl_xor(n, w);
-    if (lane == 0) before[wave] = n;
-    __syncthreads();
-    seq = before[0] + before[1] + before[2] + before[3];
-  } else if (c.cu_new != nullptr) {
-    seq = seq_of_row(c, row);
-  }
-  seq = __builtin_amdgcn_readfirstlane(seq);
-  if (seq < 0 || seq >= c.n_seqs) return;
-  const SeqRows r = rows_of_seq(c, seq);
-  if (row < r.first || row - r.first >= r.count) return;
-  const int kvh = (int)((uint32_t)h / a.group_div), i = (row - r.first) * a.group + h - kvh * a.group, jr = i % kRows;
-  const int tile_bits = part.prefix[c.n_seqs + 1];
-  const PairShape shape = pairs_of(a, teams, r, tile_bits);
-  const int round = (int)((uint32_t)i / teams.rows), member = i / kRows - round * teams.size;
-  const int t0 = part.prefix[seq] + (kvh * shape.rounds + round) * shape.tiles, each = tiles_each(part.prefix[c.n_seqs], teams.count);
-  const int w0 = (int)((uint32_t)t0 / (uint32_t)each), count = (int)((uint32_t)(t0 + shape.tiles - 1) / (uint32_t)each) - w0 + 1;
-  if (count <= 1 || t0 < 0 || w0 >= teams.count || count > teams.count - w0) return;   // finished where it was computed (or cu_new is not ascending)
+  // a row of no sequence has nothing in the workspace, and whatever it finds there stays inside it
+  const u32x2 found = part.parts[blockIdx.x];
+  if (c.cu_new != nullptr && (row < load_const(c.cu_new, 0) || row >= load_const(c.cu_new, c.n_seqs))) return;
+  const int block = (int)__builtin_amdgcn_readfirstlane(found[0]), jr = (int)__builtin_amdgcn_readfirstlane(found[1]) & 255, count = (int)(__builtin_amdgcn_readfirstlane(found[1]) >> 8);
+  if (count <= 1 || (uint32_t)block >= (uint32_t)(teams.count * teams.size) || jr >= kRows) return;   // finished where it was computed
+  const Place first = place_of(teams, block);
+  if (count > teams.count - first.team) return;
   const int team = tid / kTeam, e = tid % kTeam;
-  auto at = [&](int s) { return (2 * (int64_t)block_of(teams, w0 + s, member) + (s == 0 ? 1 : 0)) * kRows + jr; };
+  auto at = [&](int s) { return (2 * (int64_t)block_of(teams, first.team + s, first.member) + (s == 0 ? 1 : 0)) * kRows + jr; };
   f32x4 y[kBatch];
-  auto ask = [&](int first) {
+  auto ask = [&](int from) {
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const int s = first + k * kTeams + team;
+      const int s = from + k * kTeams + team;
       y[k] = s < count ? *reinterpret_cast<const f32x4*>(part.o + at(s) * kD + e * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
@@ -706,12 +684,12 @@ __global__ __launch_bounds__(256, 8) void cache_join_kernel(CacheAttnArgs a, Tea
   const float ref = top == -INFINITY ? 0.f : top;
   float sum = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int first = 0; first < count; first += kBatch * kTeams) {
-    if (first > 0) ask(first);
+  for (int from = 0; from < count; from += kBatch * kTeams) {
+    if (from > 0) ask(from);
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const int s = min(first + k * kTeams + team, count - 1);
-      const bool live = first + k * kTeams + team < count;
+      const int s = min(from + k * kTeams + team, count - 1);
+      const bool live = from + k * kTeams + team < count;
       const float f = __builtin_amdgcn_exp2f(ms[s] - ref);
       sum += live ? f * sums[s] : 0.f;
       x += live ? f * y[k] : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -784,7 +762,7 @@ double cache_attn_tiles(const CacheAttnArgs& a, int io_dtype) { return plan_of(a
 
 int64_t cache_attn_workspace_bytes(const CacheAttnArgs& a, int io_dtype) {
   const Plan p = plan_of(a, io_dtype == 0);
-  return align16(4 * ((int64_t)a.cache.n_seqs + 2)) + (int64_t)2 * p.teams * p.team_size * 16 * p.nt * 4 * (2 + a.d);
+  return align16(8 * (int64_t)a.cache.n_rows * a.Hq) + (int64_t)2 * p.teams * p.team_size * 16 * p.nt * 4 * (2 + a.d);
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t stream) {
@@ -792,8 +770,8 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t s
   const Plan p = plan_of(a, io_dtype == 0);
   Partial part;
   char* w = a.ws;
-  part.prefix = reinterpret_cast<int32_t*>(w);
-  w += align16(4 * ((int64_t)a.cache.n_seqs + 2));
+  part.parts = reinterpret_cast<u32x2*>(w);
+  w += align16(8 * (int64_t)a.cache.n_rows * a.Hq);
   const int64_t rows = (int64_t)2 * p.teams * p.team_size * 16 * p.nt;
   const Teams teams = {p.teams, p.team_size, fast_div(16 * p.nt * p.team_size)};
   part.o = reinterpret_cast<float*>(w);
