@@ -39,7 +39,7 @@ struct Partial {
 
 // Workgroups come in teams of `size` that read the same keys at the same time for different groups of rows, so that memory is read once and the others find the keys in
 // their L2: blocks b and b + 8 are on the same XCD.  rows: those of a team, size * kRows.
-struct Teams { int count, size; FastDiv rows; };
+struct Teams { int count, alone, size; FastDiv rows; };   // alone: as many as have a CU to each of their members
 struct Place { int team, member; };
 __device__ __forceinline__ Place place_of(const Teams& t, int block) {
   const int i = block >> 3, q = i / t.size;
@@ -102,26 +102,50 @@ __device__ __forceinline__ int tiles_each(int total, int n_teams) { return max(1
 // A sum that the host has ruled out comes from a cu_new that is not ascending: no tile is taken.
 __device__ __forceinline__ int checked_total(int total) { return total < 0 || total > 1 << 30 ? 0 : total; }
 
-// Keys of a tile, as a logarithm: the fewest, from a step of four wavefronts on, with which every workgroup has at most one tile, or else 256.  Smaller tiles
-// balance better, but each segment of a range costs some 4 us (28/4 heads, 64 sequences of 150 to 16384 tokens, tiles of 64 / 128 / 256 / 512 keys: 66.9 / 64.5 /
-// 62.8 / 62.6 us; 16 drafts of up to five tokens on 40 to 5003: 36 / 26 / 22.8; five f32 sequences of 1 to 1001: 5.7 / 6.6 / 8.8).
-// tiles(bits): those of this lane's sequence.
+// Keys of a tile, as a logarithm, and the teams that share the tiles out: all, two workgroups a CU, or only those that have a CU to themselves (the others leave at once).
+// Counted in keys that a CU goes through, plus 256 for each pair that a range has to begin in its middle or behind another, the cheapest of
+//   alone   one tile a workgroup, one workgroup a CU,
+//   split   the same with ranges of several tiles, as fine as they come (or coarser, where ranges still have five),
+//   shared  one tile a workgroup, two a CU, which get in each other's way (9/8);
+// if there are too many pairs for these, ranges of tiles of 256 keys for two workgroups a CU.  28/4 heads, us with 128 / 256 / 512 / 1024 keys for two workgroups a CU, and so picked:
+// 8 sequences of 5003 and three new tokens 28.4 / 27.6 / 27.6 / 24.1, 23.9 (split); 20000 and three 20.1 / 20.0 / 17.6 / 22.4, 17.9 (alone); 33 sequences of 100 to 3000 and
+// up to six 29.6 / 24.4 / 28.0 / 28.8, 25.3 (shared); 16 of 5003 and five 40.5 / 45.4 / 47.6 / 47.3, 39.6 (split).
 constexpr int kUsualBits = 8;
 constexpr int fewest_bits(bool bf16) { return bf16 ? 7 : 6; }
+struct Cut { int bits, teams; };
+// tiles(bits): those of this lane's sequence; pairs: its pairs; least: the fewest tiles of one of them, at kFewest.
 template <int kFewest, class Tiles>
-__device__ __forceinline__ int pick_tile(Tiles tiles, int n_seqs, int n_teams) {
-  constexpr int kMost = 9;
-  int n[kMost - kFewest + 1];
+__device__ __forceinline__ Cut pick_cut(Tiles tiles, int pairs, int least, int n_seqs, const Teams& teams) {
+  constexpr int kMost = 10;
+  int n[kMost - kFewest + 2];
 #pragma unroll
   for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] = min(tiles(b), 1 << 24);   // 64 of them stay below 2^31
+  n[kMost - kFewest + 1] = min(pairs, 1 << 24);
 #pragma unroll 1
-  for (int w = 1; w < n_seqs; w <<= 1)
+  for (int w = 1; w < n_seqs; w <<= 1) {
 #pragma unroll
-    for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] += __shfl_xor(n[b - kFewest], w);
-  int bits = kUsualBits;
+    for (int b = kFewest; b <= kMost + 1; ++b) n[b - kFewest] += __shfl_xor(n[b - kFewest], w);
+    least = min(least, __shfl_xor(least, w));
+  }
+  constexpr int kNever = 1 << 30;
+  int alone = kNever, shared = kNever, fine = kFewest;  // alone, shared: keys of the tile
 #pragma unroll
-  for (int b = kMost; b >= kFewest; --b) bits = n[b - kFewest] <= n_teams ? b : bits;
-  return __builtin_amdgcn_readfirstlane(bits);
+  for (int b = kMost; b >= kFewest; --b) {
+    alone = n[b - kFewest] <= teams.alone ? 1 << b : alone;
+    shared = n[b - kFewest] <= teams.count ? 1 << b : shared;
+  }
+#pragma unroll
+  for (int b = kFewest + 1; b < kMost; ++b) fine = n[b - kFewest] >= 5 * teams.alone ? b : fine;
+  const int range = tiles_each(n[0], teams.alone);
+  const int split = teams.size == 1 && n[kMost - kFewest + 1] <= teams.alone && range < 1 << 16 ? (range << kFewest) + 256 * ((range + least - 1) / least) : kNever;
+  shared = shared == kNever ? kNever : 9 * shared / 4;
+  Cut c = {kUsualBits, teams.count};
+  if (alone < kNever && alone <= split && alone <= shared) c = {31 - __builtin_clz(alone), teams.alone};
+  else if (split < kNever && split <= shared) c = {fine, teams.alone};
+  else if (shared < kNever) c.bits = 31 - __builtin_clz(shared / 2);   // 9 / 8 of the tile's keys
+  c.bits = __builtin_amdgcn_readfirstlane(c.bits);
+  c.teams = __builtin_amdgcn_readfirstlane(c.teams);
+  return c;
 }
 
 template <bool kBf16, int kD, int kNT, int kWaves>
@@ -157,12 +181,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
     const PairShape p = pairs_of(a, teams, r, bits);
     return p.rounds * a.Hkv * p.tiles;
   };
+  int n_teams = teams.count;
   const bool few = c.n_seqs <= 64;                      // every wavefront has all sequences in its lanes: no LDS, no second look at memory
   SeqRows mine = {};                                    // of sequence `lane`, if few
   int each, t, t_end, seq, base;                        // tiles of a range, the next tile, the range's end; the tile's sequence, and tiles before that one
   if (few) {
     if (lane < c.n_seqs) mine = rows_of_seq(c, lane);
-    if (tile_bits < 0) tile_bits = pick_tile<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, c.n_seqs, teams.count);
+    if (tile_bits < 0) {
+      const Cut cut = pick_cut<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, lane < c.n_seqs ? tiles_of(mine, 30) : 0,
+                                                         mine.count > 0 ? pairs_of(a, teams, mine, fewest_bits(kBf16)).tiles : 1 << 24, c.n_seqs, teams);
+      tile_bits = cut.bits;
+      n_teams = cut.teams;
+    }
     const int n = lane < c.n_seqs ? tiles_of(mine, tile_bits) : 0;
     int upto = n;
 #pragma unroll 1
@@ -171,7 +201,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       if (lane >= w) upto += x;
     }
     const int total = checked_total(__builtin_amdgcn_readlane(upto, c.n_seqs - 1));
-    each = tiles_each(total, teams.count);
+    each = tiles_each(total, n_teams);
     t = me.team * each;
     t_end = min(t + each, total);
     if (t >= t_end) return;
@@ -198,7 +228,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       total += wave_tiles[w];
     }
     total = checked_total(__builtin_amdgcn_readfirstlane(total));
-    each = tiles_each(total, teams.count);
+    each = tiles_each(total, n_teams);
     t = me.team * each;
     t_end = min(t + each, total);
     if (t >= t_end) return;
@@ -852,7 +882,7 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t s
   part.parts = reinterpret_cast<u32x2*>(w);
   w += align16(8 * (int64_t)a.cache.n_rows * a.Hq);
   const int64_t rows = (int64_t)2 * p.teams * p.team_size * 16 * p.nt;
-  const Teams teams = {p.teams, p.team_size, fast_div(16 * p.nt * p.team_size)};
+  const Teams teams = {p.teams, p.team_size == 1 ? std::min(p.teams, cu_count()) : p.teams, p.team_size, fast_div(16 * p.nt * p.team_size)};
   part.o = reinterpret_cast<float*>(w);
   part.m = part.o + rows * a.d;
   part.l = part.m + rows;
