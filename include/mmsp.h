@@ -293,7 +293,7 @@ typedef struct {
   int64_t tok_stride, head_stride;   /* >= head_dim, multiples of 8                        */
 } mmsp_heads;
 
-/* y[t] = x[t] turned, for rows [0, n_rows) of n_tensors (1 or 2: Q and K) tensors with the same number
+/* y[t] = x[t] turned, for rows [0, n_rows), n_rows <= 2^26, of n_tensors (1 or 2: Q and K) tensors with the same number
  * of heads on both sides.  positions (device, int32, may be negative): position of row r on axis a at
  * [a * pos_stride + r].  inverse != 0 turns back, which is the gradient of the forward: dX from dY.
  * The arithmetic is fp32 and rounded once.  dtypes: both sides the same, or f32 to bf16 (gradients); the tensors
@@ -309,7 +309,7 @@ mmsp_status mmsp_rotary_apply(const mmsp_rotary* rotary, int64_t n_rows, const i
  * mmsp_attn_merge.  Entries behind a sequence's last token are of no account.
  * New tokens: rows [cu_new[s], cu_new[s+1]) of Q (and of K, V in mmsp_cache_append) are the last tokens of
  * sequence s, that is row cu_new[s] + i is its token lengths[s] - n_new + i.  cu_new == NULL: one new
- * token each, n_rows == n_seqs.  Rows from cu_new[n_seqs] on are padding and stay as they are.  A row whose token number is
+ * token each, n_rows == n_seqs.  Rows before cu_new[0] and from cu_new[n_seqs] on are padding and stay as they are.  A row whose token number is
  * negative sees nothing and is not written to the cache.  Lengths beyond max_pages * page_size count as that
  * many.  page_table, lengths and cu_new are read by the kernels, so a captured graph follows their contents. */
 typedef struct {
@@ -347,7 +347,7 @@ size_t mmsp_cache_workspace_bytes(const mmsp_shape* shape, const mmsp_cache* cac
  * NaN or infinity included, has no influence.  A NaN in a V that a row sees gives a NaN in that element of O, an infinity gives an infinity or a NaN there.
  * q: [n_rows, n_q_heads, d] with the shape's q strides (its kv strides are not used).  Results, each may be NULL, not
  * all: o_final dense [n_rows, n_q_heads, d] in io_dtype; o the same in f32, for mmsp_attn_merge; lse
- * [n_q_heads][lse_head_stride].  Meant for one or a few new tokens per sequence (any number is right; a
+ * [n_q_heads][lse_head_stride]; they do not overlap the inputs.  Meant for one or a few new tokens per sequence (any number is right; a
  * whole prompt is faster through mmsp_attn_step_fwd).  UNSUPPORTED where n_rows * n_q_heads exceeds 2^23, or
  * sequences x KV heads x capacity (max_pages * page_size) some 2^36 tokens.  Results are bit-identical from run to run on one kind of device.
  * workspace: at least mmsp_cache_workspace_bytes() bytes, 16-byte aligned; its contents need not be set and

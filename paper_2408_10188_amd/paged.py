@@ -35,14 +35,17 @@ def cache_for(k_pool, v_pool, page_table=None, lengths=None, n_rows=0, cu_new=No
     """mmsp_cache for pools [n_pages, n_kv_heads, page_size, d], page_table [n_seqs, max_pages], lengths [n_seqs] and
     cu_new [n_seqs + 1] (int32, on the pool's device)."""
     import torch
-    if k_pool.dim() != 4 or k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() or k_pool.stride(3) != 1 or k_pool.dtype != v_pool.dtype:
-        raise ValueError("two pools [n_pages, n_kv_heads, page_size, d] of the same type and strides, d contiguous, are wanted")
+    if (k_pool.dim() != 4 or k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() or k_pool.stride(3) != 1 or k_pool.dtype != v_pool.dtype
+            or k_pool.device != v_pool.device):
+        raise ValueError("two pools [n_pages, n_kv_heads, page_size, d] of the same type, strides and device, d contiguous, are wanted")
     for name, t, dims in (("page_table", page_table, 2), ("lengths", lengths, 1), ("cu_new", cu_new, 1)):
         if t is not None and (t.dtype != torch.int32 or t.dim() != dims or t.stride(-1) != 1 or t.device != k_pool.device):
             raise ValueError("%s must be int32 with %d dimensions, contiguous, on the pool's device" % (name, dims))
     n_seqs = 0 if lengths is None else len(lengths)
     if page_table is not None and len(page_table) != n_seqs or cu_new is not None and len(cu_new) != n_seqs + 1:
         raise ValueError("page_table, lengths and cu_new must have n_seqs, n_seqs and n_seqs + 1 entries")
+    if page_table is not None and n_seqs > 1 and page_table.stride(0) < page_table.shape[1]:
+        raise ValueError("the rows of page_table must not overlap (an expanded one has to be copied)")
     pages, heads, page_size, d = k_pool.shape
     # a size of one may have any stride
     strides = (k_pool.stride(0) if pages > 1 else heads * page_size * d, k_pool.stride(2), k_pool.stride(1) if heads > 1 else page_size * d)
@@ -85,7 +88,8 @@ class PagedCache:
     def free(self, seq):
         B.mmsp_pages_free(self.pages, self.rows[seq], self.lengths[seq])
         del self.rows[seq], self.lengths[seq]
-        self._step = None
+        if self._step is not None and seq in self._step[4]:
+            self._step = None
 
     def _copy(self, copies):
         import torch
@@ -132,7 +136,7 @@ class PagedCache:
         lengths = torch.tensor([self.lengths[s] for s in seqs], dtype=torch.int32, device=dev)
         cu_new = None if all(n == 1 for n in n_new) else torch.from_numpy(np.concatenate([[0], np.cumsum(n_new)]).astype(np.int32)).to(dev)
         self._copy(copies)
-        self._step = (table, lengths, cu_new, int(sum(n_new)))
+        self._step = (table, lengths, cu_new, int(sum(n_new)), frozenset(seqs))
         self._ws = None
 
     def _undo(self, seq, n, before):
@@ -148,7 +152,7 @@ class PagedCache:
     def _cache(self, layer):
         if self._step is None:
             raise RuntimeError("step() comes first")
-        table, lengths, cu_new, n_rows = self._step
+        table, lengths, cu_new, n_rows, _ = self._step
         return cache_for(self.k[layer], self.v[layer], table, lengths, n_rows, cu_new)
 
     def _shape(self, q, k=None, scale=1.0):
@@ -172,9 +176,9 @@ class PagedCache:
             raise ValueError("q_out must be contiguous, or q itself")
         if q.shape[1:] != (self.n_q_heads, self.k.shape[-1]) or k.shape[1:] != (self.k.shape[2], self.k.shape[-1]):
             raise ValueError("Q and K must have the cache's heads")
-        if rotary is not None and (positions is None or positions.dtype != torch.int32 or positions.shape != (rotary.n_axes, n) or positions.stride(1) != 1
-                                   or positions.device != self.k.device):
-            raise ValueError("positions must be int32 [%d, %d] on the pool's device" % (rotary.n_axes, n))
+        if rotary is not None and (positions is None or positions.dtype != torch.int32 or positions.shape != (rotary.n_axes, n) or n > 1 and positions.stride(1) != 1
+                                   or rotary.n_axes > 1 and positions.stride(0) < n or positions.device != self.k.device):
+            raise ValueError("positions must be int32 [%d, %d] on the pool's device, contiguous, the axes apart (expanded ones have to be copied)" % (rotary.n_axes, n))
         if n == 0:
             return q_out
         with torch.cuda.device(self.k.device):

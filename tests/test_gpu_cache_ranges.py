@@ -78,3 +78,26 @@ def test_numbers_of_rows_around_the_layouts(new, dtype):
     lengths = [n + 100 + 517 * (i % 3) for i, n in enumerate(new)]
     Problem(23, lengths, new, dtype=dtype, hq=14, hkv=2, page=16, pad_rows=len(new) % 2).check()
     Problem(24, [n + 3000 for n in new], new, dtype=dtype, hq=7, hkv=1, page=64).check()
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("lengths", [[5003] * 16, [100 + 9 * i * i % 2900 for i in range(33)], [30 + 1291 * i % 4000 for i in range(64)]], ids=["even", "33", "64"])
+def test_cuts_of_batches(lengths, dtype, d):
+    """Ranges of several tiles for one workgroup a CU, one tile for each of two, and pairs of very different lengths in a range."""
+    Problem(25, lengths, dtype=dtype, d=d, hq=8, hkv=4, page=64).check()
+
+
+@pytest.mark.parametrize("first", [0, 4])
+def test_rows_before_the_first_sequence(first):
+    """The rows of a call may begin anywhere: what lies before cu_new[0] and behind cu_new[n_seqs] is left alone, by the joining launch too."""
+    whole = Problem(26, [4000, 3, 900], [3, 1, 2], hq=14, hkv=2, page=64, pad_rows=7)
+    want = whole.run()
+    q = torch.roll(whole.q, first, 0).contiguous()
+    cu = whole.dev["cu_new"] + first
+    cache = paged.cache_for(whole.k, whole.v, whole.dev["page_table"], whole.dev["lengths"], whole.n_rows, cu)
+    got = [torch.full_like(t, math.nan) for t in want]
+    B.mmsp_cache_attn(whole.shape, cache, q, *got, whole.ws, whole.ws_bytes)
+    for a, b in zip(want, got):
+        a, b = (a, b) if a.shape[0] == whole.n_rows else (a.T, b.T)
+        assert torch.equal(a[:6], b[first:first + 6])
+        assert bool(torch.isnan(b[:first]).all()) and bool(torch.isnan(b[first + 6:]).all())

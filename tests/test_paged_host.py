@@ -41,7 +41,7 @@ def test_steps_take_pages_all_or_none():
     a, b = c.add(), c.add()
     c.step([a, b], [40, 16])
     assert c.rows[a].tolist() == [0, 1, 2, -1, -1, -1, -1] and c.rows[b][:2].tolist() == [3, -1] and c.lengths == {a: 40, b: 16}
-    table, lengths, cu_new, n = c._step
+    table, lengths, cu_new, n = c._step[:4]
     assert table.tolist() == [c.rows[a].tolist(), c.rows[b].tolist()] and lengths.tolist() == [40, 16] and cu_new.tolist() == [0, 40, 56] and n == 56
     c.step([b], [1])
     assert c._step[2] is None and c.rows[b][:2].tolist() == [3, 4]
@@ -82,14 +82,15 @@ def test_layers_of_the_python_side_refuse_wrong_tensors():
                dict(q_out=wide[:, :4]), dict(q=wide[:, :4], q_out=wide.view(-1)[:3 * 512].view(3, 4, 128))):
         with pytest.raises(ValueError):
             c.append(0, rot, pos, **{**good, **kw})
-    for p in (None, pos[:2], pos.long(), torch.zeros(3, 4, dtype=torch.int32), pos.to("meta")):
+    for p in (None, pos[:2], pos.long(), torch.zeros(3, 4, dtype=torch.int32), pos.to("meta"), pos[:1].expand(3, 3), pos.T):
         with pytest.raises(ValueError):
             c.append(0, rot, p, **good)
     for kw in (dict(q=bf(3, 2, 128)), dict(o_final=torch.zeros(3, 4, 128)), dict(o=bf(3, 4, 128)), dict(o_final=wide[:, :4]), dict(lse=torch.zeros(4, 4)), dict(q=bf(3, 4, 128).to("meta"))):
         with pytest.raises(ValueError):
             c.attend(0, **{**dict(q=bf(3, 4, 128)), **kw})
     pool = torch.zeros(4, 2, 16, 128)
-    for bad in (dict(v_pool=pool.bfloat16()), dict(v_pool=pool[:3]), dict(page_table=torch.zeros(1, 2)), dict(lengths=torch.zeros(1)),
+    for bad in (dict(v_pool=pool.bfloat16()), dict(v_pool=pool[:3]), dict(v_pool=pool.to("meta")),
+                dict(page_table=torch.zeros(1, 2, dtype=torch.int32).expand(3, 2), lengths=torch.zeros(3, dtype=torch.int32)), dict(page_table=torch.zeros(1, 2)), dict(lengths=torch.zeros(1)),
                 dict(page_table=torch.zeros(2, 2, dtype=torch.int32), lengths=torch.zeros(1, dtype=torch.int32)),
                 dict(lengths=torch.zeros(2, dtype=torch.int32), cu_new=torch.zeros(2, dtype=torch.int32))):
         with pytest.raises(ValueError):
@@ -99,6 +100,17 @@ def test_layers_of_the_python_side_refuse_wrong_tensors():
         paged.heads_of(torch.zeros(3, 128, 4).transpose(1, 2))
     with pytest.raises(ValueError):
         paged.heads_of(torch.zeros(3, 4, 128, dtype=torch.float16))
+
+
+def test_a_sequence_that_goes_ends_the_step_it_is_in():
+    c = _cache()
+    a, b = c.add(), c.add()
+    c.step([b], [3])
+    c.free(a)
+    assert c._cache(0).n_rows == 3
+    c.free(b)
+    with pytest.raises(RuntimeError):
+        c._cache(0)
 
 
 def test_a_step_without_tokens_does_nothing():
