@@ -77,6 +77,12 @@ class MmspError(RuntimeError):
 if not os.path.exists(LIB_PATH):
     raise ImportError("libmmsp.so is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "
                       "(or python paper_2408_10188_amd/build.py) first; there is no fallback path")
+try:
+    # torch brings a HIP runtime of its own, which the library shares if it is there first; loaded the other way round there are two in the
+    # process, and the one behind the library sees no device.
+    import torch  # noqa: F401
+except ImportError:
+    pass
 _lib = ctypes.CDLL(LIB_PATH)
 
 _P, _I64, _I32, _INT, _SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_size_t

@@ -2,6 +2,7 @@
 import ctypes
 import os
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -26,6 +27,13 @@ def test_structures_are_laid_out_as_in_the_header(tmp_path):
         assert int(said[name]) == ctypes.sizeof(s)
         for f, _ in s._fields_:
             assert int(said["%s.%s" % (name, f)]) == getattr(s, f).offset, (name, f)
+
+
+@pytest.mark.parametrize("first", ["from paper_2408_10188_amd import binding", "import torch"])
+def test_one_hip_runtime_in_whatever_order(first):
+    """The library and torch share one, also where the binding is imported before torch."""
+    code = first + "\nimport torch\nfrom paper_2408_10188_amd import binding\nprint(len({line.split()[-1] for line in open('/proc/self/maps') if 'libamdhip64' in line}))"
+    assert subprocess.run([sys.executable, "-c", code], cwd=ROOT, check=True, capture_output=True, text=True).stdout.split() == ["1"]
 
 
 def _cache(n_pages=12, page=16, max_tokens=100):
