@@ -102,49 +102,50 @@ __device__ __forceinline__ int tiles_each(int total, int n_teams) { return max(1
 // A sum that the host has ruled out comes from a cu_new that is not ascending: no tile is taken.
 __device__ __forceinline__ int checked_total(int total) { return total < 0 || total > 1 << 30 ? 0 : total; }
 
-// Keys of a tile, as a logarithm, and the teams that share the tiles out: all, two workgroups a CU, or only those that have a CU to themselves (the others leave at once).
-// Counted in keys that a CU goes through, plus 256 for each pair that a range has to begin in its middle or behind another, the cheapest of
-//   alone   one tile a workgroup, one workgroup a CU,
-//   split   the same with ranges of several tiles, as fine as they come (or coarser, where ranges still have five),
-//   shared  one tile a workgroup, two a CU, which get in each other's way (9/8);
-// if there are too many pairs for these, ranges of tiles of 256 keys for two workgroups a CU.  28/4 heads, us with 128 / 256 / 512 / 1024 keys for two workgroups a CU, and so picked:
-// 8 sequences of 5003 and three new tokens 28.4 / 27.6 / 27.6 / 24.1, 23.9 (split); 20000 and three 20.1 / 20.0 / 17.6 / 22.4, 17.9 (alone); 33 sequences of 100 to 3000 and
-// up to six 29.6 / 24.4 / 28.0 / 28.8, 25.3 (shared); 16 of 5003 and five 40.5 / 45.4 / 47.6 / 47.3, 39.6 (split).
-constexpr int kUsualBits = 8;
+// How the tiles of a call are shared out: keys of a tile, as a logarithm; teams, all of them, two workgroups a CU, or only those that have a CU to themselves (the others
+// leave at once); and how many tiles a pair counts for beside its own, where ranges hold several pairs, each of which costs some 2 us to begin and to end.
+struct Cut { int bits, teams, extra; };
 constexpr int fewest_bits(bool bf16) { return bf16 ? 7 : 6; }
-struct Cut { int bits, teams; };
-// tiles(bits): those of this lane's sequence; pairs: its pairs; least: the fewest tiles of one of them, at kFewest.
+constexpr int kExtra = 2;
+// With many pairs: ranges of the smallest tiles for two workgroups a CU, one of which computes while the other begins or ends a pair.  28/4 heads, 200 sequences of 50 to 8000
+// and up to four new tokens, us with tiles of 256 keys, no extra tiles / 256 and one / 128 and two / three: 127 / 114 / 112 / 115; 70 of 100 to 16000 and one: 89.7 / 84.1 /
+// 84.6 / 85.2; 200 of 2000 and one: 134.6 / 133.1 / 135.1 / 136.1.
+__device__ __forceinline__ Cut usual_cut(int fewest, const Teams& teams) { return {fewest, teams.count, kExtra}; }
+// Counted in keys that a CU goes through, the cheapest of
+//   alone   one tile a workgroup, one workgroup a CU,
+//   split   ranges of several of the smallest tiles, one workgroup a CU,
+//   shared  one tile a workgroup, two a CU, which get in each other's way (9/8).
+// 28/4 heads, us with tiles of 128 / 256 / 512 / 1024 keys for two workgroups a CU, and so picked: 20000 keys and three new tokens 20.1 / 20.0 / 17.6 / 22.4, 17.9 (alone);
+// 8 sequences of 5003 and three 28.4 / 27.6 / 27.6 / 24.1, 23.9 (split); 16 of 5003 and five 40.5 / 45.4 / 47.6 / 47.3, 39.8 (split); 64 of 150 to 16384 and one
+// 66.8 / 67.1 / 65.7 / -, 64.6 (split; pairs without extra tiles 67.6); 33 of 100 to 3000 and up to six 29.6 / 24.4 / 28.0 / 28.8, 25.3 (shared).
+// tiles(bits): those of this lane's sequence; pairs: its pairs.
 template <int kFewest, class Tiles>
-__device__ __forceinline__ Cut pick_cut(Tiles tiles, int pairs, int least, int n_seqs, const Teams& teams) {
-  constexpr int kMost = 10;
+__device__ __forceinline__ Cut pick_cut(Tiles tiles, int pairs, int n_seqs, const Teams& teams) {
+  constexpr int kMost = 10, kNever = 1 << 30;
   int n[kMost - kFewest + 2];
 #pragma unroll
   for (int b = kFewest; b <= kMost; ++b) n[b - kFewest] = min(tiles(b), 1 << 24);   // 64 of them stay below 2^31
-  n[kMost - kFewest + 1] = min(pairs, 1 << 24);
+  int& all_pairs = n[kMost - kFewest + 1];
+  all_pairs = min(pairs, 1 << 22);
 #pragma unroll 1
-  for (int w = 1; w < n_seqs; w <<= 1) {
+  for (int w = 1; w < n_seqs; w <<= 1)
 #pragma unroll
     for (int b = kFewest; b <= kMost + 1; ++b) n[b - kFewest] += __shfl_xor(n[b - kFewest], w);
-    least = min(least, __shfl_xor(least, w));
-  }
-  constexpr int kNever = 1 << 30;
-  int alone = kNever, shared = kNever, fine = kFewest;  // alone, shared: keys of the tile
+  int alone = kNever, shared = kNever, split = kNever;  // keys
 #pragma unroll
   for (int b = kMost; b >= kFewest; --b) {
     alone = n[b - kFewest] <= teams.alone ? 1 << b : alone;
-    shared = n[b - kFewest] <= teams.count ? 1 << b : shared;
+    shared = n[b - kFewest] <= teams.count ? 9 << b >> 2 : shared;
   }
-#pragma unroll
-  for (int b = kFewest + 1; b < kMost; ++b) fine = n[b - kFewest] >= 5 * teams.alone ? b : fine;
-  const int range = tiles_each(n[0], teams.alone);
-  const int split = teams.size == 1 && n[kMost - kFewest + 1] <= teams.alone && range < 1 << 16 ? (range << kFewest) + 256 * ((range + least - 1) / least) : kNever;
-  shared = shared == kNever ? kNever : 9 * shared / 4;
-  Cut c = {kUsualBits, teams.count};
-  if (alone < kNever && alone <= split && alone <= shared) c = {31 - __builtin_clz(alone), teams.alone};
-  else if (split < kNever && split <= shared) c = {fine, teams.alone};
-  else if (shared < kNever) c.bits = 31 - __builtin_clz(shared / 2);   // 9 / 8 of the tile's keys
+  const int extra = 8 * all_pairs <= teams.alone ? 0 : kExtra;   // long pairs: few ranges hold two (256K keys: 87.0 instead of 88.0 us)
+  if (teams.size == 1 && all_pairs <= teams.alone) split = min(tiles_each(n[0] + extra * all_pairs, teams.alone), 1 << 20) << kFewest;
+  Cut c = usual_cut(kFewest, teams);
+  if (alone < kNever && alone <= split && alone <= shared) c = {31 - __builtin_clz(alone), teams.alone, 0};
+  else if (split < kNever && split <= shared) c = {kFewest, teams.alone, extra};
+  else if (shared < kNever) c = {30 - __builtin_clz(shared), teams.count, 0};
   c.bits = __builtin_amdgcn_readfirstlane(c.bits);
   c.teams = __builtin_amdgcn_readfirstlane(c.teams);
+  c.extra = __builtin_amdgcn_readfirstlane(c.extra);
   return c;
 }
 
@@ -177,9 +178,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
   // ---- this team's range of tiles ----
   const Place me = place_of(teams, blockIdx.x);
   // (Every bound below also holds where cu_new is not ascending and the sums are nonsense.)
+  int extra = 0;                                        // a pair counts as so many tiles more than it has
   auto tiles_of = [&](const SeqRows& r, int bits) {
     const PairShape p = pairs_of(a, teams, r, bits);
-    return p.rounds * a.Hkv * p.tiles;
+    return p.rounds * a.Hkv * (p.tiles + extra);
   };
   int n_teams = teams.count;
   const bool few = c.n_seqs <= 64;                      // every wavefront has all sequences in its lanes: no LDS, no second look at memory
@@ -189,9 +191,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
     if (lane < c.n_seqs) mine = rows_of_seq(c, lane);
     if (tile_bits < 0) {
       const Cut cut = pick_cut<fewest_bits(kBf16)>([&](int bits) { return lane < c.n_seqs ? tiles_of(mine, bits) : 0; }, lane < c.n_seqs ? tiles_of(mine, 30) : 0,
-                                                         mine.count > 0 ? pairs_of(a, teams, mine, fewest_bits(kBf16)).tiles : 1 << 24, c.n_seqs, teams);
+                                                   c.n_seqs, teams);
       tile_bits = cut.bits;
       n_teams = cut.teams;
+      extra = cut.extra;
     }
     const int n = lane < c.n_seqs ? tiles_of(mine, tile_bits) : 0;
     int upto = n;
@@ -208,7 +211,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
     seq = 63 - __builtin_clzll(__ballot(lane < c.n_seqs && upto - n <= t) | 1);   // the last one that begins by then
     base = __builtin_amdgcn_readlane(upto - n, seq);
   } else {
-    if (tile_bits < 0) tile_bits = kUsualBits;
+    if (tile_bits < 0) {
+      const Cut cut = usual_cut(fewest_bits(kBf16), teams);
+      tile_bits = cut.bits;
+      extra = cut.extra;
+    }
     const int per = (c.n_seqs + kThreads - 1) / kThreads, s_first = min(tid * per, c.n_seqs), s_last = min(s_first + per, c.n_seqs);
     int n = 0;
     for (int s = s_first; s < s_last; ++s) n += tiles_of(rows_of_seq(c, s), tile_bits);
@@ -266,16 +273,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArg
       r.length = __builtin_amdgcn_readfirstlane(r.length);
     }
     const PairShape shape = pairs_of(a, teams, r, tile_bits);
-    const int n_seq = shape.rounds * a.Hkv * shape.tiles;
+    const int span = shape.tiles + extra, n_seq = shape.rounds * a.Hkv * span;
     if (t >= base + n_seq) { base += n_seq; ++seq; continue; }
-    const int pair = (int)((uint32_t)(t - base) / (uint32_t)shape.tiles);
-    const int tile0 = __builtin_amdgcn_readfirstlane(t - base - pair * shape.tiles);
+    const int pair = (int)((uint32_t)(t - base) / (uint32_t)span);
+    const int tile0 = __builtin_amdgcn_readfirstlane(t - base - pair * span);
     const int tile1 = __builtin_amdgcn_readfirstlane(min(shape.tiles, tile0 + (t_end - t)));
     const int kvh = __builtin_amdgcn_readfirstlane((int)((uint32_t)pair / (uint32_t)shape.rounds));
     const int group0 = __builtin_amdgcn_readfirstlane(((pair - kvh * shape.rounds) * teams.size + me.member) * kRows);
     // teams that have tiles of this pair, from the one with its first tile on
     const int n_parts = __builtin_amdgcn_readfirstlane((int)((uint32_t)(t - tile0 + shape.tiles - 1) / (uint32_t)each) - me.team + 1);
-    t += tile1 - tile0;
+    t += min(span - tile0, t_end - t);
+    if (tile0 >= shape.tiles) continue;                 // nothing but what the pair counts for
 
     // ---- rows ----
     const int n_list = r.count * a.group, first_pos = r.length - r.count;
@@ -857,7 +865,7 @@ Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   p.waves = p.nt == 1 && (p.shared ? pairs * 8 <= n_cu : pairs <= n_cu) ? 8 : 4;
   p.tile_bits = p.shared ? -1 : 30;
   const int fewest = 1 << fewest_bits(bf16);
-  p.most = pairs * (p.shared ? (double)((capacity + fewest - 1) / fewest) : 1.);
+  p.most = pairs * (p.shared ? (double)((capacity + fewest - 1) / fewest + kExtra) : 1.);
   p.teams = (int)std::min<double>(std::min(kMaxGroups, n_cu * (p.waves == 4 ? 2 : 1)) / p.team_size, p.most);
   if (p.team_size > 1) p.teams = (p.teams + 7) / 8 * 8;  // all blocks of a team exist
   return p;
