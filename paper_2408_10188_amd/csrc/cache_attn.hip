@@ -3,7 +3,7 @@
 //
 // Work.  The (token, head) pairs of a KV head's new rows are one list, as in the forward kernel; groups of kRows of it are
 // stationary, 16, 32 or 48 of them.  A pair of (sequence, KV head, group) has the sequence's keys in tiles.  The tiles of all pairs are one sequence that is cut
-// into as many equal ranges as there are workgroups, whatever the lengths are: a workgroup goes through the segments
+// into as many equal ranges as there are workgroups (or half as many, see pick_cut), whatever the lengths are: a workgroup goes through the segments
 // of pairs in its range.  A pair inside one range is finished there; at most the first and the last segment of a range are
 // parts of pairs that others share: their (O, maximum, sum) goes to the workspace and a second launch joins them.  The lengths are on the device only,
 // so each workgroup adds up the tiles of all sequences for itself.
@@ -15,8 +15,10 @@
 // slots so that the accumulators of S^T are B operands as they are, and a lane's V pieces (8 elements of d of the 8 keys of its
 // slots) become the A operands of 8 products by exchanging halves of registers.
 //
-// Measured, 28/4 heads, one token, both launches: 203 tokens 6.8 us (a chain: lengths, pages and Q, K and V, the results), 256K tokens 87 us, of which the loop reads
-// 6.9 TB/s (a plain read of that size 7.1), 64 sequences of 150 to 16384 tokens 67 us.
+// Teams.  Where a sequence has more rows than a group takes, workgroups on one XCD take a group each and read the same keys at the same time (Teams).
+//
+// Measured, 28/4 heads, one token, both launches: 203 tokens 6.9 us (a chain: lengths, pages and Q, K and V, the results), 256K tokens 87 us, of which the loop reads
+// 6.9 TB/s (a plain read of that size 7.1), 64 sequences of 150 to 16384 tokens 64.4 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -149,9 +151,9 @@ __device__ __forceinline__ Cut pick_cut(Tiles tiles, int pairs, int n_seqs, cons
   return c;
 }
 
-template <bool kBf16, int kD, int kNT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 2) void cache_attn_kernel(CacheAttnArgs a, Teams teams, int tile_bits, Partial part) {
-  constexpr int kThreads = 64 * kWaves;
+template <bool kBf16, int kD, int kNT>
+__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Teams teams, int tile_bits, Partial part) {
+  constexpr int kWaves = 4, kThreads = 64 * kWaves;
   constexpr int kRows = 16 * kNT, kElt = kBf16 ? 2 : 4;
   constexpr int kBlocks = kBf16 ? 2 : 1, kKeys = 16 * kBlocks;   // blocks of 16 keys, keys of a step
   constexpr int kKL = kD * kElt / 64;                   // 16-byte pieces of a K row that a lane holds
@@ -830,9 +832,9 @@ __global__ __launch_bounds__(256, 8) void cache_join_rows_kernel(CacheAttnArgs a
   if (team == 0) store_result<kBf16, kD>(a, row_head, e, x, sum, ref);
 }
 
-// How a call is laid out: tiles of 16 rows of a workgroup's group, wavefronts of a workgroup, teams and their members, the logarithm of a tile's keys (-1: picked by the
+// How a call is laid out: tiles of 16 rows of a workgroup's group, teams and their members, the logarithm of a tile's keys (-1: picked by the
 // kernel), and whether several workgroups may share a pair.
-struct Plan { int nt, waves, team_size, teams, tile_bits; bool shared; double most; };   // most: tiles of all pairs at most
+struct Plan { int nt, team_size, teams, tile_bits; bool shared; double most; };   // most: tiles of all pairs at most
 Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   const CacheArgs& c = a.cache;
   const int n_cu = cu_count();
@@ -856,17 +858,15 @@ Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   p.team_size = (int)std::min<int64_t>(kMaxTeam, workgroups(p.nt));
   const int64_t capacity = (int64_t)c.max_pages * c.page_size;
   const double pairs = (double)(rows_all / (16 * p.nt * p.team_size) + c.n_seqs) * a.Hkv;
-  // A short cache: one workgroup for a pair, and no second launch.  28/4 heads, us so and with shared pairs: 8 sequences of 400 tokens 9.5 and 11.4, of
-  // 900 14.1 and 11.7; 60 of 900 21.4 and 27.7, 200 of 900 64.5 and 75.7, of 20 to 900 39.0 and 37.9, of 1900 138.0 and 138.9.
-  p.shared = capacity > (pairs * 2 >= n_cu ? 1024 : 512) / (bf16 ? 1 : 2);
-  // Eight wavefronts and a CU to itself, or four and half a CU.  Eight take a pair in half the time and leave half as many partial results (one sequence of 256K
-  // tokens: 87.2 instead of 89.7 us); of two workgroups on a CU one computes while the other starts or ends a segment (64 sequences of 150 to 16384: 68.8 instead
-  // of 63.2).
-  p.waves = p.nt == 1 && (p.shared ? pairs * 8 <= n_cu : pairs <= n_cu) ? 8 : 4;
+  // A short cache: one workgroup for a pair, and no second launch, up to 512 tokens (f32 half of that), or 1024 for pairs that fill the chip once.  28/4 heads, one new token,
+  // us so and with shared pairs: 8 sequences of 450 tokens 9.9 and 11.5, of 900 14.9 and 12.3; 60 of 900 22.2 and 25.2, of 20 to 900 14.9 and 16.2; 200 of 450 34.7 and
+  // 39.3, of 900 64.7 and 67.6, of 20 to 900 40.0 and 31.1 (with five new tokens each, of 900, 77.3 and 90.4).
+  const bool once = pairs * 2 >= n_cu && (pairs <= 2.5 * n_cu || p.nt > 1);
+  p.shared = capacity > (once ? 1024 : 512) / (bf16 ? 1 : 2);
   p.tile_bits = p.shared ? -1 : 30;
   const int fewest = 1 << fewest_bits(bf16);
   p.most = pairs * (p.shared ? (double)((capacity + fewest - 1) / fewest + kExtra) : 1.);
-  p.teams = (int)std::min<double>(std::min(kMaxGroups, n_cu * (p.waves == 4 ? 2 : 1)) / p.team_size, p.most);
+  p.teams = (int)std::min<double>(std::min(kMaxGroups, 2 * n_cu) / p.team_size, p.most);
   if (p.team_size > 1) p.teams = (p.teams + 7) / 8 * 8;  // all blocks of a team exist
   return p;
 }
@@ -894,10 +894,10 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t s
   part.o = reinterpret_cast<float*>(w);
   part.m = part.o + rows * a.d;
   part.l = part.m + rows;
-  auto launch = [&](auto bf16, auto d, auto nt, auto waves) {
+  auto launch = [&](auto bf16, auto d, auto nt) {
     constexpr bool kBf16 = decltype(bf16)::value;
-    constexpr int kD = decltype(d)::value, kNT = decltype(nt)::value, kWaves = decltype(waves)::value;
-    cache_attn_kernel<kBf16, kD, kNT, kWaves><<<dim3((unsigned)(p.teams * p.team_size)), dim3(64 * kWaves), 0, stream>>>(a, teams, p.tile_bits, part);
+    constexpr int kD = decltype(d)::value, kNT = decltype(nt)::value;
+    cache_attn_kernel<kBf16, kD, kNT><<<dim3((unsigned)(p.teams * p.team_size)), dim3(256), 0, stream>>>(a, teams, p.tile_bits, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.shared || p.teams == 1) return e;
     const int n = a.cache.n_rows * a.Hq;
@@ -908,12 +908,10 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int io_dtype, hipStream_t s
     return hipGetLastError();
   };
   auto by_rows = [&](auto bf16, auto d) {
-    using four = std::integral_constant<int, 4>;
     if constexpr (decltype(bf16)::value)
-      if (p.nt == 3) return launch(bf16, d, std::integral_constant<int, 3>(), four());
-    if (p.nt == 2) return launch(bf16, d, std::integral_constant<int, 2>(), four());
-    if (p.waves == 4) return launch(bf16, d, std::integral_constant<int, 1>(), four());
-    return launch(bf16, d, std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+      if (p.nt == 3) return launch(bf16, d, std::integral_constant<int, 3>());
+    if (p.nt == 2) return launch(bf16, d, std::integral_constant<int, 2>());
+    return launch(bf16, d, std::integral_constant<int, 1>());
   };
   if (io_dtype == 0) return by_rows(std::true_type(), std::integral_constant<int, 128>());
   if (a.d == 128) return by_rows(std::false_type(), std::integral_constant<int, 128>());
