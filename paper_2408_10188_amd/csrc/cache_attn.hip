@@ -41,7 +41,7 @@ struct Partial {
 
 // Workgroups come in teams of `size` that read the same keys at the same time for different groups of rows, so that memory is read once and the others find the keys in
 // their L2: blocks b and b + 8 are on the same XCD.  rows: those of a team, size * kRows.
-struct Teams { int count, alone, size; FastDiv rows; };   // alone: as many as have a CU to each of their members
+struct Teams { int count, alone, size; FastDiv rows; };   // alone: for teams of one, as many as have a CU to themselves; else all
 struct Place { int team, member; };
 __device__ __forceinline__ Place place_of(const Teams& t, int block) {
   const int i = block >> 3, q = i / t.size;
@@ -115,7 +115,7 @@ constexpr int kExtra = 2;
 __device__ __forceinline__ Cut usual_cut(int fewest, const Teams& teams) { return {fewest, teams.count, kExtra}; }
 // Counted in keys that a CU goes through, the cheapest of
 //   alone   one tile a workgroup, one workgroup a CU,
-//   split   ranges of several of the smallest tiles, one workgroup a CU,
+//   split   ranges of several of the smallest tiles, one workgroup a CU (teams of several: two; one costs those with idle members up to 15 %),
 //   shared  one tile a workgroup, two a CU, which get in each other's way (9/8).
 // 28/4 heads, us with tiles of 128 / 256 / 512 / 1024 keys for two workgroups a CU, and so picked: 20000 keys and three new tokens 20.1 / 20.0 / 17.6 / 22.4, 17.9 (alone);
 // 8 sequences of 5003 and three 28.4 / 27.6 / 27.6 / 24.1, 23.9 (split); 16 of 5003 and five 40.5 / 45.4 / 47.6 / 47.3, 39.8 (split); 64 of 150 to 16384 and one
@@ -140,7 +140,7 @@ __device__ __forceinline__ Cut pick_cut(Tiles tiles, int pairs, int n_seqs, cons
     shared = n[b - kFewest] <= teams.count ? 9 << b >> 2 : shared;
   }
   const int extra = 8 * all_pairs <= teams.alone ? 0 : kExtra;   // long pairs: few ranges hold two (256K keys: 87.0 instead of 88.0 us)
-  if (teams.size == 1 && all_pairs <= teams.alone) split = min(tiles_each(n[0] + extra * all_pairs, teams.alone), 1 << 20) << kFewest;
+  if (all_pairs <= teams.alone) split = min(tiles_each(n[0] + extra * all_pairs, teams.alone), 1 << 20) << kFewest;
   Cut c = usual_cut(kFewest, teams);
   if (alone < kNever && alone <= split && alone <= shared) c = {31 - __builtin_clz(alone), teams.alone, 0};
   else if (split < kNever && split <= shared) c = {kFewest, teams.alone, extra};
