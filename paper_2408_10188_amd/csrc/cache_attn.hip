@@ -838,15 +838,12 @@ struct Plan { int nt, team_size, teams, tile_bits; bool shared; double most; }; 
 Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   const CacheArgs& c = a.cache;
   const int n_cu = cu_count();
-  // Rows of a sequence: the same number each if that can be.  Else twice the mean for the teams, whose members have nothing to do for a sequence with fewer, and 2.5 times
-  // the mean, which few will exceed, for the rows of a group (16 drafts of up to five tokens on 40 to 5003, 28/4 heads: groups of 32 27.2 us, of 48 23.6;
-  // 100 with up to four on 100 to 2000, whose rows fit 32: 34.2 and 37.3).
-  const int64_t rows_all = (int64_t)c.n_rows * a.group;
-  const bool even = c.n_rows % c.n_seqs == 0;
-  const int64_t rows_each = std::max<int64_t>(1, (even ? 1 : 2) * rows_all / c.n_seqs), rows_most = even ? rows_each : 5 * rows_all / (2 * (int64_t)c.n_seqs);
+  // Rows of a sequence: the same number each if that can be, or else twice the mean, which few exceed by much.  (With 2.5 times: 16 drafts of up to five tokens on 40 to 5003,
+  // 28/4 heads, of which some have 35 rows, 22.1 instead of 22.9 us, but 100 with up to four on 100 to 2000, whose rows fit 32, 36.3 instead of 33.5.)
+  const int64_t rows_all = (int64_t)c.n_rows * a.group, rows_each = std::max<int64_t>(1, (c.n_rows % c.n_seqs == 0 ? 1 : 2) * rows_all / c.n_seqs);
   // Groups of 32 rows, or of 48 (bf16) where they need fewer workgroups, in teams of a power of two (three members do not find each other's keys).  28/4 heads, 16
-  // sequences of 20000 keys, us with groups of 48 / of 32: 5 new tokens 122 / 144, 9 148 / 150, 13 167 / 222, 16 257 / 228, 20 261 / 352, 32 467 / 364; without teams 9
-  // took 222, 16 342.
+  // sequences of 20000 keys, us with groups of 48 / of 32: 5 new tokens 112 / 141, 9 157 / 143, 13 160 / 213, 16 244 / 215, 20 246 / 342, 32 454 / 350; as picked, but without
+  // teams: 9 214, 16 401, 32 733.
   auto workgroups = [&](int nt) {
     const int64_t groups = (rows_each + 16 * nt - 1) / (16 * nt);
     int64_t n = 1;
@@ -854,7 +851,7 @@ Plan plan_of(const CacheAttnArgs& a, bool bf16) {
     return (groups + n - 1) / n * n;
   };
   Plan p;
-  p.nt = rows_most <= 16 ? 1 : rows_most <= 32 ? 2 : bf16 && (rows_most <= 48 || workgroups(3) < workgroups(2)) ? 3 : 2;
+  p.nt = rows_each <= 16 ? 1 : bf16 && workgroups(3) < workgroups(2) ? 3 : 2;
   p.team_size = (int)std::min<int64_t>(kMaxTeam, workgroups(p.nt));
   const int64_t capacity = (int64_t)c.max_pages * c.page_size;
   const double pairs = (double)(rows_all / (16 * p.nt * p.team_size) + c.n_seqs) * a.Hkv;
