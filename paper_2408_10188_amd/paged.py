@@ -132,7 +132,9 @@ class PagedCache:
         for s, n in zip(seqs, n_new):
             self.lengths[s] += n
         dev = self.k.device
-        table = torch.from_numpy(np.stack([self.rows[s] for s in seqs]) if seqs else np.zeros((0, self.max_pages), dtype=np.int32)).to(dev)
+        # as wide as the longest of them: the calls lay their work out for that many tokens
+        width = max([1] + [-(-self.lengths[s] // self.page_size) for s in seqs])
+        table = torch.from_numpy(np.stack([self.rows[s][:width] for s in seqs]) if seqs else np.zeros((0, width), dtype=np.int32)).to(dev)
         lengths = torch.tensor([self.lengths[s] for s in seqs], dtype=torch.int32, device=dev)
         cu_new = None if all(n == 1 for n in n_new) else torch.from_numpy(np.concatenate([[0], np.cumsum(n_new)]).astype(np.int32)).to(dev)
         self._copy(copies)
