@@ -159,6 +159,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
   constexpr int kKL = kD * kElt / 64;                   // 16-byte pieces of a K row that a lane holds
   constexpr int kVC = kD * kElt / 256;                  // .. of a V row
   constexpr int kAcc = kD / 16;                         // O^T accumulators of 16 rows of d
+  constexpr int kParts = kNT == 1 ? 3 : 2;              // bf16 numbers that a weight is given to the matrix instructions as
   constexpr int kHalf = kKeys * kD * kElt, kCopies = kHalf / 1024;   // bytes of a step's K (or V), copies that bring them
   // A wavefront's K and V of a step; when a segment ends, the wavefronts' O for kAtOnce tiles of 16 rows, [kAtOnce][kWaves][16][kD] floats, each row's pieces of 4 in
   // places piece ^ row.
@@ -458,21 +459,27 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
           }
       }
 
-      // O^T += V^T . P^T.  P goes in as two bf16 numbers, its rounding and what that leaves: 16 bits together, so that a partial result is as
-      // exact as the fp32 it is kept in; the second product costs nothing where memory sets the pace.
-      bf16x8 p_hi[kNT], p_lo[kNT];
+      // O^T += V^T . P^T.  P goes in as two or three bf16 numbers, its rounding and what that leaves: 16 bits or all 24 of it.  V's are exact, so with three a partial
+      // result is as exact as the fp32 it is kept in: O before its rounding is off by 1.5e-7 to 5e-7 of its size (203 to 262144 keys; 1.6e-6 to 2.1e-6 with two).  With one
+      // tile of rows memory sets the pace and the third product is all but free (28/4 heads, one new token, us with two and three: 256K tokens 87.3 and 87.4, 16 sequences
+      // of 20000 106.3 and 107.4, 8 of 450 9.9 and 10.1); with more tiles it is not (16 of 20000, five tokens 113.6 and 120.3, 32 tokens 349 and 392).
+      bf16x8 p_part[kNT][kParts];
       if constexpr (kBf16) {
 #pragma unroll
         for (int j = 0; j < kNT; ++j) {
-          uint32_t hi_w[4], lo_w[4];
+          uint32_t w[kParts][4];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float p0 = p[j][w >> 1][(w & 1) * 2], p1 = p[j][w >> 1][(w & 1) * 2 + 1];
-            hi_w[w] = pack2(p0, p1);
-            lo_w[w] = pack2(p0 - __uint_as_float(hi_w[w] << 16), p1 - __uint_as_float(hi_w[w] & 0xffff0000u));
+          for (int y = 0; y < 4; ++y) {
+            float p0 = p[j][y >> 1][(y & 1) * 2], p1 = p[j][y >> 1][(y & 1) * 2 + 1];
+#pragma unroll
+            for (int x2 = 0; x2 < kParts; ++x2) {
+              w[x2][y] = pack2(p0, p1);
+              p0 -= __uint_as_float(w[x2][y] << 16);     // exact
+              p1 -= __uint_as_float(w[x2][y] & 0xffff0000u);
+            }
           }
-          p_hi[j] = __builtin_bit_cast(bf16x8, mk4(hi_w[0], hi_w[1], hi_w[2], hi_w[3]));
-          p_lo[j] = __builtin_bit_cast(bf16x8, mk4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]));
+#pragma unroll
+          for (int x2 = 0; x2 < kParts; ++x2) p_part[j][x2] = __builtin_bit_cast(bf16x8, mk4(w[x2][0], w[x2][1], w[x2][2], w[x2][3]));
         }
       }
       if (more) wait_copies<kCopies>();                  // the next step's K is under way
@@ -558,8 +565,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
 #pragma unroll
         for (int j = 0; j < kNT; ++j) {
           if constexpr (kBf16) {
-            acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_hi[j], acc[j][e], 0, 0, 0);
-            acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_lo[j], acc[j][e], 0, 0, 0);
+#pragma unroll
+            for (int x2 = 0; x2 < kParts; ++x2) acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p_part[j][x2], acc[j][e], 0, 0, 0);
           } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i], p[j][0][i], acc[j][e], 0, 0, 0);
