@@ -310,8 +310,8 @@ mmsp_status mmsp_rotary_apply(const mmsp_rotary* rotary, int64_t n_rows, const i
  * New tokens: rows [cu_new[s], cu_new[s+1]) of Q (and of K, V in mmsp_cache_append) are the last tokens of
  * sequence s, that is row cu_new[s] + i is its token lengths[s] - n_new + i.  cu_new == NULL: one new
  * token each, n_rows == n_seqs.  Rows before cu_new[0] and from cu_new[n_seqs] on are padding and stay as they are.  A row whose token number is
- * negative sees nothing and is not written to the cache.  Lengths beyond max_pages * page_size count as that
- * many.  page_table, lengths and cu_new are read by the kernels, so a captured graph follows their contents. */
+ * negative sees nothing and is not written to the cache.  Tokens from max_pages * page_size on, of a length beyond that, are nowhere: they are neither written nor
+ * seen, and no other token changes its number for them.  page_table, lengths and cu_new are read by the kernels, so a captured graph follows their contents. */
 typedef struct {
   void* k; void* v;          /* device, 16-byte aligned: [n_pages][..] in io_dtype         */
   int64_t page_stride, tok_stride, head_stride;   /* elements, of K and of V; >= head_dim, multiples of 8 */

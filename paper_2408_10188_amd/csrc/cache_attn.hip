@@ -268,11 +268,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
     if (few) {
       r.first = __builtin_amdgcn_readlane(mine.first, seq);
       r.count = __builtin_amdgcn_readlane(mine.count, seq);
+      r.token = __builtin_amdgcn_readlane(mine.token, seq);
       r.length = __builtin_amdgcn_readlane(mine.length, seq);
     } else {
       r = rows_of_seq(c, seq);
       r.first = __builtin_amdgcn_readfirstlane(r.first);
       r.count = __builtin_amdgcn_readfirstlane(r.count);
+      r.token = __builtin_amdgcn_readfirstlane(r.token);
       r.length = __builtin_amdgcn_readfirstlane(r.length);
     }
     const PairShape shape = pairs_of(a, teams, r, tile_bits);
@@ -289,7 +291,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
     if (tile0 >= shape.tiles) continue;                 // nothing but what the pair counts for
 
     // ---- rows ----
-    const int n_list = r.count * a.group, first_pos = r.length - r.count;
+    const int n_list = r.count * a.group;
+    auto last_key = [&](int tok) { return min(r.token + tok, r.length - 1); };   // that new token `tok` sees
     if (group0 >= n_list) continue;                     // fewer groups than the team has members
     int hi[kNT];                                        // last key that this lane's rows see
     u32x4 q[kSharedQ ? 1 : kNT][kKL];
@@ -297,7 +300,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
     for (int j = 0; j < kNT; ++j) {
       const int i = group0 + j * 16 + col, ic = min(i, n_list - 1);
       const int tok = (int)((uint32_t)ic / a.group_div);
-      hi[j] = first_pos + tok;                          // a row behind the last one does as that one
+      hi[j] = last_key(tok);                            // a row behind the last one does as that one
       const char* p = reinterpret_cast<const char*>(a.q) + ((int64_t)(r.first + tok) * a.q_ts + (kvh * a.group + ic - tok * a.group) * a.q_hs) * kElt + quad * 16;
       if (kSharedQ && wave != j) continue;
 #pragma unroll
@@ -308,8 +311,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
     }
     static_assert(!kSharedQ || (kNT <= kWaves && kD * kElt == 256), "a wavefront for each 16 rows of Q, 16 pieces a row");
     if constexpr (kSharedQ) __syncthreads();
-    const int hi_max = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)(min(group0 + kRows, n_list) - 1) / a.group_div));
-    const int hi_min = __builtin_amdgcn_readfirstlane(first_pos + (int)((uint32_t)group0 / a.group_div));
+    const int hi_max = __builtin_amdgcn_readfirstlane(last_key((int)((uint32_t)(min(group0 + kRows, n_list) - 1) / a.group_div)));
+    const int hi_min = __builtin_amdgcn_readfirstlane(last_key((int)((uint32_t)group0 / a.group_div)));
     const int key_end = __builtin_amdgcn_readfirstlane(min((int)min((int64_t)tile1 << tile_bits, (int64_t)INT32_MAX), hi_max + 1));
 
     bool odd = false;                                   // this lane has left out an infinity or NaN of V

@@ -20,16 +20,22 @@ __device__ __forceinline__ T load_const(const T* p, int64_t i) {
   return ((const __attribute__((address_space(4))) T*)(uintptr_t)p)[i];
 }
 
-// The new rows [first, first + count) of sequence s, and its length.  Whatever the device arrays hold, rows stay inside the row
-// buffers and lengths inside the page table.
-struct SeqRows { int first, count, length; };
+// The new rows [first, first + count) of sequence s, the token of the first of them, and the tokens that the page table has room for.  Whatever the device arrays hold,
+// rows stay inside the row buffers and tokens below `length` inside the page table.  Token numbers go by the length as given: new tokens behind the table's end are nowhere,
+// they do not take the numbers of those before it.
+struct SeqRows { int first, count, token, length; };
 __device__ __forceinline__ SeqRows rows_of_seq(const CacheArgs& c, int s) {
   SeqRows r;
-  const int capacity = c.max_pages * c.page_size;
-  r.length = min(max(load_const(c.lengths, s), 0), capacity);
-  if (c.cu_new == nullptr) { r.first = s; r.count = 1; return r; }
-  r.first = min(max(load_const(c.cu_new, s), 0), c.n_rows);
-  r.count = min(max(load_const(c.cu_new, s + 1), r.first), c.n_rows) - r.first;
+  const int length = max(load_const(c.lengths, s), 0);
+  r.length = min(length, c.max_pages * c.page_size);
+  if (c.cu_new == nullptr) {
+    r.first = s;
+    r.count = 1;
+  } else {
+    r.first = min(max(load_const(c.cu_new, s), 0), c.n_rows);
+    r.count = min(max(load_const(c.cu_new, s + 1), r.first), c.n_rows) - r.first;
+  }
+  r.token = length - r.count;
   return r;
 }
 // The sequence of row r, -1 behind the last one: the first s with r < cu_new[s + 1].

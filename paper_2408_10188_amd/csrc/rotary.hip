@@ -183,8 +183,8 @@ __global__ __launch_bounds__(256) void append_kernel(RotaryArgs rot, AppendArgs 
         int64_t at = -1;
         if (seq >= 0) {
           const SeqRows s = rows_of_seq(a.cache, seq);
-          const int token = s.length - s.count + row - s.first;
-          if (token >= 0 && token < s.length) {
+          const int token = s.token + row - s.first;
+          if (token >= 0 && token < s.length) {          // behind the table's end: not written
             const int p = (int)((uint32_t)token / a.cache.page_div), page = a.cache.table[seq * a.cache.table_stride + p];
             if (page >= 0 && page < a.cache.n_pages) at = page * a.cache.page_stride + (token - p * a.cache.page_size) * a.cache.tok_stride;
           }

@@ -101,3 +101,42 @@ def test_rows_before_the_first_sequence(first):
         a, b = (a, b) if a.shape[0] == whole.n_rows else (a.T, b.T)
         assert torch.equal(a[:6], b[first:first + 6])
         assert bool(torch.isnan(b[:first]).all()) and bool(torch.isnan(b[first + 6:]).all())
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+def test_new_tokens_behind_the_tables_end(dtype, d):
+    """Lengths that have gone past the page tables (48 tokens), by one, by a few, as far as an int32 goes: those tokens are nowhere.  None of the tokens that are there is
+    written over, and the new ones before the end keep their numbers, in the append and in the attention."""
+    page, hkv, room = 16, 2, 48
+    lengths, new = [49, 50, 48, 2 ** 31 - 1, 60], [1, 4, 2, 5, 12]
+    cu = [0, 1, 5, 7, 12, 24]
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    k_pool, v_pool = (torch.randn(15, hkv, page, d, device=DEV, generator=gen).to(dtype) for _ in range(2))
+    q, k, v = (torch.randn(cu[-1], h, d, device=DEV, generator=gen).to(dtype) for h in (4, hkv, hkv))
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    table, seen = torch.arange(15, device=DEV, dtype=torch.int32).view(5, 3), dev(lengths)
+    for per_seq in (True, False):                           # one new token each, then the ragged numbers
+        n_rows = 5 if per_seq else cu[-1]
+        starts = None if per_seq else dev(cu)
+        cache = paged.cache_for(k_pool, v_pool, table, seen, n_rows, starts)
+        shape = B.make_shape(4, hkv, d, B.MMSP_F32 if dtype == F32 else B.MMSP_BF16, 0.1, (4 * d, d), (hkv * d, d), n_rows)
+        rows = [(s, s, lengths[s] - 1) for s in range(5)] if per_seq else [(cu[s] + i, s, lengths[s] - new[s] + i) for s in range(5) for i in range(new[s])]
+        want = k_pool.clone(), v_pool.clone()
+        for r, s, token in rows:
+            if token < room:
+                for pool, x in zip(want, (k, v)):
+                    pool[3 * s + token // page, :, token % page] = x[r]
+        B.mmsp_cache_append(shape, cache, None, None, 0, None, k, v)
+        assert torch.equal(k_pool, want[0]) and torch.equal(v_pool, want[1])
+        # what each row sees, as sequences of their own whose only new token is the row
+        o, lse = torch.full((n_rows, 4, d), math.nan, device=DEV), torch.full((4, n_rows), math.nan, device=DEV)
+        ws = torch.empty(B.mmsp_cache_workspace_bytes(shape, cache), dtype=torch.uint8, device=DEV)
+        B.mmsp_cache_attn(shape, cache, q, None, o, lse, ws, len(ws))
+        alone_table, alone = table[torch.tensor([s for _, s, _ in rows], device=DEV)].contiguous(), dev([min(token + 1, room) for _, _, token in rows])
+        shape = B.make_shape(4, hkv, d, shape.io_dtype, 0.1, (4 * d, d), (hkv * d, d), n_rows)
+        cache = paged.cache_for(k_pool, v_pool, alone_table, alone, n_rows)
+        want_o, want_lse = torch.full_like(o, math.nan), torch.full_like(lse, math.nan)
+        ws = torch.empty(B.mmsp_cache_workspace_bytes(shape, cache), dtype=torch.uint8, device=DEV)
+        B.mmsp_cache_attn(shape, cache, q, None, want_o, want_lse, ws, len(ws))
+        # both sum at most 48 terms in fp32, weights with 16 bits at least: a row that sees a key more or less is off by far more (a weight of 1/48 or so)
+        assert bool(((o - want_o).abs() <= 1e-4).all()) and bool(((lse - want_lse).abs() <= 1e-5).all())
