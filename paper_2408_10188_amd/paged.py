@@ -113,7 +113,8 @@ class PagedCache:
 
     def step(self, seqs, n_new):
         """The next n_new[i] tokens of sequences seqs[i], whose rows of Q, K and V come one sequence after the other.  Takes the
-        pages for them; raises MmspError (status MMSP_ERR_NO_PAGES) with nothing changed where the pool has too few."""
+        pages for them; raises MmspError (status MMSP_ERR_NO_PAGES) where the pool has too few.  A call that raises, for whatever
+        reason, has changed nothing: the step before it is still the present one."""
         import torch
         if len(set(seqs)) != len(seqs) or len(seqs) != len(n_new) or min(n_new, default=0) < 0:
             raise ValueError("every sequence once, with a number of new tokens")
@@ -125,19 +126,19 @@ class PagedCache:
                 done.append((s, n, before))
                 if copy is not None:
                     copies.append(copy)
-        except Exception:
-            for s, n, before in reversed(done):           # what was taken is given back
+            dev = self.k.device
+            after = [self.lengths[s] + n for s, n in zip(seqs, n_new)]
+            # as wide as the longest of them: the calls lay their work out for that many tokens
+            width = max([1] + [-(-n // self.page_size) for n in after])
+            table = torch.from_numpy(np.stack([self.rows[s][:width] for s in seqs]) if seqs else np.zeros((0, width), dtype=np.int32)).to(dev)
+            lengths = torch.tensor(after, dtype=torch.int32, device=dev)
+            cu_new = None if all(n == 1 for n in n_new) else torch.from_numpy(np.concatenate([[0], np.cumsum(n_new)]).astype(np.int32)).to(dev)
+            self._copy(copies)
+        except BaseException:
+            for s, n, before in reversed(done):           # what was taken is given back; copies into it, if some were made, change nothing that is held
                 self._undo(s, n, before)
             raise
-        for s, n in zip(seqs, n_new):
-            self.lengths[s] += n
-        dev = self.k.device
-        # as wide as the longest of them: the calls lay their work out for that many tokens
-        width = max([1] + [-(-self.lengths[s] // self.page_size) for s in seqs])
-        table = torch.from_numpy(np.stack([self.rows[s][:width] for s in seqs]) if seqs else np.zeros((0, width), dtype=np.int32)).to(dev)
-        lengths = torch.tensor([self.lengths[s] for s in seqs], dtype=torch.int32, device=dev)
-        cu_new = None if all(n == 1 for n in n_new) else torch.from_numpy(np.concatenate([[0], np.cumsum(n_new)]).astype(np.int32)).to(dev)
-        self._copy(copies)
+        self.lengths.update(zip(seqs, after))
         self._step = (table, lengths, cu_new, int(sum(n_new)), frozenset(seqs))
         self._ws = None
 

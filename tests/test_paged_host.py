@@ -142,3 +142,30 @@ def test_calls_too_large_for_a_grid_are_refused():
     with pytest.raises(B.MmspError) as e:                                   # 2^22 layers of K and V of 512 pieces of 16 bytes: 2^32 threads
         B.mmsp_cache_copy_pages(shape, cache(1, 1), 1 << 22, 8, 4096, 1)
     assert e.value.status == B.MMSP_ERR_UNSUPPORTED
+
+
+def _fails(*args, **kw):
+    raise MemoryError("no room on the device")
+
+
+@pytest.mark.parametrize("what", ["the copies", "the table", "the lengths"])
+def test_a_step_whose_device_work_fails_changes_nothing(what, monkeypatch):
+    """Where the uploads or the page copies raise, no page has been taken and no length moved; the next step makes the copy that this one did not."""
+    c = _cache()
+    a = c.add()
+    c.step([a], [20])
+    b = c.fork(a)                                        # its second page is partly filled and shared
+    before, step = _state(c), c._step
+    with monkeypatch.context() as m:
+        if what == "the copies":
+            m.setattr(c, "_copy", _fails)
+        else:
+            m.setattr(torch, "from_numpy" if what == "the table" else "tensor", _fails)
+        with pytest.raises(MemoryError):
+            c.step([b, a], [30, 1])
+    assert _state(c) == before and c._step is step
+    assert sorted(c._free[:c.pages.n_free].tolist()) == [i for i, r in enumerate(before[0]) if r == 0]
+    made = []
+    monkeypatch.setattr(c, "_copy", made.extend)
+    c.step([b], [1])
+    assert made == [(1, c.rows[b][1], 4)] and c.rows[b][1] not in before[2][a] and c.lengths == {a: 20, b: 21}
