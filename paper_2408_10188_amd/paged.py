@@ -101,14 +101,19 @@ class PagedCache:
             B.mmsp_cache_copy_pages(shape, cache, len(self.k), self.k.stride(0), dev, len(copies), torch.cuda.current_stream().cuda_stream)
 
     def compact(self):
-        """Moves the pages in use to the front of the pool; returns how many there are."""
+        """Moves the pages in use to the front of the pool; returns how many there are.  Where the copies cannot be made it raises, and no page has moved."""
         names = list(self.rows)
         table = np.stack([self.rows[s] for s in names]) if names else np.zeros((0, self.max_pages), dtype=np.int32)
+        before = self._refs.copy(), self._free.copy(), self.pages.n_free
         copies, used = B.mmsp_pages_compact(self.pages, table, np.array([self.lengths[s] for s in names], dtype=np.int64))
+        try:
+            self._copy(copies)
+        except BaseException:                             # copies that were made went into free pages
+            self._refs[:], self._free[:], self.pages.n_free = before
+            raise
         for s, row in zip(names, table):
             self.rows[s][:] = row
         self._step = None
-        self._copy(copies)
         return used
 
     def step(self, seqs, n_new):

@@ -169,3 +169,22 @@ def test_a_step_whose_device_work_fails_changes_nothing(what, monkeypatch):
     monkeypatch.setattr(c, "_copy", made.extend)
     c.step([b], [1])
     assert made == [(1, c.rows[b][1], 4)] and c.rows[b][1] not in before[2][a] and c.lengths == {a: 20, b: 21}
+
+
+def test_a_compaction_whose_copies_fail_moves_nothing(monkeypatch):
+    c = _cache()
+    a, b = c.add(), c.add()
+    c.step([a, b], [40, 20])
+    c.free(a)
+    c.step([b], [1])
+    before, free, step = _state(c), c._free.tolist(), c._step
+    with monkeypatch.context() as m:
+        m.setattr(c, "_copy", _fails)
+        with pytest.raises(MemoryError):
+            c.compact()
+    assert _state(c) == before and c._free.tolist() == free and c._step is step
+    made = []
+    monkeypatch.setattr(c, "_copy", lambda copies: made.extend(copies.tolist()))
+    assert c.compact() == 2 and made == [[3, 0, 16], [4, 1, 16]] and c.rows[b][:2].tolist() == [0, 1]
+    with pytest.raises(RuntimeError):
+        c._cache(0)
