@@ -56,7 +56,7 @@ class MmspCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("page_table", ctypes.c_void_p),
                 ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("lengths", ctypes.c_void_p),
-                ("cu_new", ctypes.c_void_p), ("n_rows", ctypes.c_int32)]
+                ("cu_new", ctypes.c_void_p), ("n_rows", ctypes.c_int32), ("most_new", ctypes.c_int32)]
 
 
 class MmspPageCopy(ctypes.Structure):
@@ -252,10 +252,10 @@ def make_heads(data, n_heads, dtype, tok_stride, head_stride):
     return MmspHeads(_ptr(data), n_heads, dtype, tok_stride, head_stride)
 
 
-def make_cache(k, v, strides, n_pages, page_size, page_table=None, table_stride=0, max_pages=0, n_seqs=0, lengths=None, cu_new=None, n_rows=0):
-    """strides = (page, token, head) in elements, of K and of V."""
+def make_cache(k, v, strides, n_pages, page_size, page_table=None, table_stride=0, max_pages=0, n_seqs=0, lengths=None, cu_new=None, n_rows=0, most_new=0):
+    """strides = (page, token, head) in elements, of K and of V; most_new: the most new tokens of a sequence, if it is known."""
     return MmspCache(_ptr(k), _ptr(v), strides[0], strides[1], strides[2], n_pages, page_size, _ptr(page_table), table_stride, max_pages, n_seqs,
-                     _ptr(lengths), _ptr(cu_new), n_rows)
+                     _ptr(lengths), _ptr(cu_new), n_rows, most_new)
 
 
 def mmsp_rotary_plan(head_dim, theta, sections):

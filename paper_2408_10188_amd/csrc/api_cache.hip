@@ -65,6 +65,7 @@ mmsp_status check_cache(const mmsp_shape* s, const mmsp_cache* c) {
     return fail(MMSP_ERR_INVALID_ARG, "max_pages=%d x page_size=%d is not in [1, 2^30] tokens", c->max_pages, c->page_size);
   if (c->n_seqs < 0 || c->n_rows < 0 || c->n_rows > kMaxRows || c->n_seqs > kMaxRows)
     return fail(MMSP_ERR_INVALID_ARG, "n_seqs=%d and n_rows=%d must be in [0, 2^26]", c->n_seqs, c->n_rows);
+  if (c->most_new < 0) return fail(MMSP_ERR_INVALID_ARG, "most_new=%d is negative", c->most_new);
   if (c->cu_new == nullptr && c->n_rows != c->n_seqs)
     return fail(MMSP_ERR_INVALID_ARG, "without cu_new every sequence has one row: n_rows=%d, n_seqs=%d", c->n_rows, c->n_seqs);
   if (c->n_seqs > 0 && (c->page_table == nullptr || c->lengths == nullptr))
@@ -78,7 +79,7 @@ CacheArgs cache_args(const mmsp_cache* c) {
   a.k = reinterpret_cast<char*>(c->k); a.v = reinterpret_cast<char*>(c->v);
   a.page_stride = c->page_stride; a.tok_stride = c->tok_stride; a.head_stride = c->head_stride;
   a.table = c->page_table; a.table_stride = c->table_stride; a.lengths = c->lengths; a.cu_new = c->cu_new;
-  a.n_pages = c->n_pages; a.page_size = c->page_size; a.max_pages = c->max_pages; a.n_seqs = c->n_seqs; a.n_rows = c->n_rows;
+  a.n_pages = c->n_pages; a.page_size = c->page_size; a.max_pages = c->max_pages; a.n_seqs = c->n_seqs; a.n_rows = c->n_rows; a.most_new = c->most_new;
   a.page_div = fast_div(c->page_size);
   return a;
 }

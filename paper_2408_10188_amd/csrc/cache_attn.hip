@@ -848,9 +848,13 @@ struct Plan { int nt, team_size, teams, tile_bits; bool shared; double most; }; 
 Plan plan_of(const CacheAttnArgs& a, bool bf16) {
   const CacheArgs& c = a.cache;
   const int n_cu = cu_count();
-  // Rows of a sequence: the same number each if that can be, or else twice the mean, which few exceed by much.  (With 2.5 times: 16 drafts of up to five tokens on 40 to 5003,
-  // 28/4 heads, of which some have 35 rows, 22.1 instead of 22.9 us, but 100 with up to four on 100 to 2000, whose rows fit 32, 36.3 instead of 33.5.)
-  const int64_t rows_all = (int64_t)c.n_rows * a.group, rows_each = std::max<int64_t>(1, (c.n_rows % c.n_seqs == 0 ? 1 : 2) * rows_all / c.n_seqs);
+  // Rows of a sequence: those of the one with the most where the host knows it (one new token each, one sequence, most_new), but at most twice the mean, which few exceed by much.
+  // (With 2.5 times: 16 drafts of up to five tokens on 40 to 5003, 28/4 heads, of which some have 35 rows, 22.1 instead of 22.9 us, but 100 with up to four on 100 to
+  // 2000, whose rows fit 32, 36.3 instead of 33.5.)  28/4 heads, us laid out for the mean, for twice the mean, and with most_new: ragged numbers, 100 sequences of 100 to 2000, up to four,
+  // 46.1 / 36.4 / 36.4; 200 of 50 to 8000, up to four, 148.7 / 106.9 / 107.2; 64 of 100 to 4000, up to six, 48.0 / 41.6 / 41.7; 16 of 2000 to 20000, up to 16, 83.6 / 99.0 / 99.2;
+  // five each, 16 of 20000, 113.6 / 148.5 / 113.9; 16 each 212 / 344 / 212.
+  const int64_t rows_all = (int64_t)c.n_rows * a.group, most = c.cu_new == nullptr ? 1 : c.most_new > 0 ? c.most_new : c.n_rows;
+  const int64_t rows_each = std::max<int64_t>(1, std::min(most * a.group, c.n_seqs == 1 ? rows_all : 2 * rows_all / c.n_seqs));
   // Groups of 32 rows, or of 48 (bf16) where they need fewer workgroups, in teams of a power of two (three members do not find each other's keys).  28/4 heads, 16
   // sequences of 20000 keys, us with groups of 48 / of 32: 5 new tokens 112 / 141, 9 157 / 143, 13 160 / 213, 16 244 / 215, 20 246 / 342, 32 454 / 350; as picked, but without
   // teams: 9 214, 16 401, 32 733.

@@ -11,6 +11,7 @@ struct CacheArgs {
   const int32_t* lengths;
   const int32_t* cu_new;                                // nullptr: one new token per sequence
   int32_t n_pages, page_size, max_pages, n_seqs, n_rows;
+  int32_t most_new;                                     // of a sequence, with cu_new; 0: not known
   FastDiv page_div;                                     // tokens / page_size
 };
 

@@ -31,9 +31,10 @@ def shape_for(k_pool, io_dtype, n_q_heads=None, n_rows=0, scale=1.0):
     return B.make_shape(hq, hkv, d, io_dtype, scale, (hq * d, d), (hkv * d, d), n_rows)
 
 
-def cache_for(k_pool, v_pool, page_table=None, lengths=None, n_rows=0, cu_new=None):
+def cache_for(k_pool, v_pool, page_table=None, lengths=None, n_rows=0, cu_new=None, most_new=0):
     """mmsp_cache for pools [n_pages, n_kv_heads, page_size, d], page_table [n_seqs, max_pages], lengths [n_seqs] and
-    cu_new [n_seqs + 1] (int32, on the pool's device)."""
+    cu_new [n_seqs + 1] (int32, on the pool's device).  most_new: the most new tokens of a sequence, where cu_new is given and the host
+    knows it; the attention is laid out by it (without it for up to twice the mean, which costs where all have the same number)."""
     import torch
     if (k_pool.dim() != 4 or k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() or k_pool.stride(3) != 1 or k_pool.dtype != v_pool.dtype
             or k_pool.device != v_pool.device):
@@ -51,7 +52,7 @@ def cache_for(k_pool, v_pool, page_table=None, lengths=None, n_rows=0, cu_new=No
     strides = (k_pool.stride(0) if pages > 1 else heads * page_size * d, k_pool.stride(2), k_pool.stride(1) if heads > 1 else page_size * d)
     width = 0 if page_table is None else page_table.shape[1]
     return B.make_cache(k_pool, v_pool, strides, pages, page_size, page_table, max(width, page_table.stride(0)) if width else 0, width, n_seqs, lengths,
-                        cu_new, n_rows)
+                        cu_new, n_rows, most_new)
 
 
 class PagedCache:
@@ -144,7 +145,7 @@ class PagedCache:
                 self._undo(s, n, before)
             raise
         self.lengths.update(zip(seqs, after))
-        self._step = (table, lengths, cu_new, int(sum(n_new)), frozenset(seqs))
+        self._step = (table, lengths, cu_new, int(sum(n_new)), frozenset(seqs), int(max(n_new, default=0)))
         self._ws = None
 
     def _undo(self, seq, n, before):
@@ -160,8 +161,8 @@ class PagedCache:
     def _cache(self, layer):
         if self._step is None:
             raise RuntimeError("step() comes first")
-        table, lengths, cu_new, n_rows, _ = self._step
-        return cache_for(self.k[layer], self.v[layer], table, lengths, n_rows, cu_new)
+        table, lengths, cu_new, n_rows, _, most_new = self._step
+        return cache_for(self.k[layer], self.v[layer], table, lengths, n_rows, cu_new, most_new)
 
     def _shape(self, q, k=None, scale=1.0):
         d = self.k.shape[-1]

@@ -256,3 +256,41 @@ def test_pages_elsewhere_are_left_alone():
 def pages_next(free, pages):
     """The page that was given out last."""
     return int(free[pages.n_free])
+
+
+# ---- the layout of the attention ----
+
+def _room(n_seqs, n_rows, most_new=0, cu_new=FAKE):
+    """Bytes of partial results: they go by the rows of a group and the number of workgroups, the layout of the call."""
+    shape = _shape(n_q_heads=28, n_kv_heads=4, q_strides=(3584, 128), kv_strides=(512, 128), lse_head_stride=n_rows)
+    cache = _cache(page_size=64, max_pages=400, table_stride=400, n_seqs=n_seqs, n_rows=n_rows, cu_new=cu_new, most_new=most_new)
+    return B.mmsp_cache_workspace_bytes(shape, cache) - -(-8 * n_rows * 28 // 16) * 16
+
+
+def test_layouts_do_not_go_by_divisibility():
+    """A total that the number of sequences happens to divide says nothing about the numbers of each."""
+    assert _room(16, 31) == _room(16, 32) == _room(16, 33)
+    assert _room(64, 191) == _room(64, 192) == _room(64, 193)
+    assert _room(16, 79) == _room(16, 80) == _room(16, 81)
+
+
+def test_layouts_go_by_the_most_new_tokens_of_a_sequence():
+    one = _room(16, 16, cu_new=None)
+    for pad in (0, 3, 16):                                  # padding rows change nothing where the number is known
+        assert _room(16, 16 + pad, most_new=1) == one
+        assert _room(16, 80 + pad, most_new=5) == _room(16, 80, most_new=5) == _room(1, 5) == _room(1, 5 + pad, most_new=5)
+    assert _room(16, 32, most_new=2) == one != _room(16, 32)   # 14 rows a KV head, not 28
+    assert _room(16, 80, most_new=500) == _room(16, 80)      # one long sequence among short ones: twice the mean at most
+    assert _room(1, 40) == _room(1, 40, most_new=40)
+    _refused(B.MMSP_ERR_INVALID_ARG, B.mmsp_cache_attn, _shape(), _cache(cu_new=FAKE, most_new=-1), FAKE, FAKE, None, None, FAKE, 1 << 40)
+
+
+def test_a_step_says_how_many_new_tokens_its_sequences_have():
+    import torch
+    from paper_2408_10188_amd import paged
+    c = paged.PagedCache(1, 12, 16, 4, 2, 128, 100, torch.bfloat16, "cpu")
+    a, b = c.add(), c.add()
+    c.step([a, b], [3, 5])
+    assert c._cache(0).most_new == 5
+    c.step([a], [1])
+    assert c._cache(0).most_new == 1
