@@ -40,7 +40,7 @@ def cache_for(k_pool, v_pool, page_table=None, lengths=None, n_rows=0, cu_new=No
             or k_pool.device != v_pool.device):
         raise ValueError("two pools [n_pages, n_kv_heads, page_size, d] of the same type, strides and device, d contiguous, are wanted")
     for name, t, dims in (("page_table", page_table, 2), ("lengths", lengths, 1), ("cu_new", cu_new, 1)):
-        if t is not None and (t.dtype != torch.int32 or t.dim() != dims or t.stride(-1) != 1 or t.device != k_pool.device):
+        if t is not None and (t.dtype != torch.int32 or t.dim() != dims or t.shape[-1] > 1 and t.numel() > 0 and t.stride(-1) != 1 or t.device != k_pool.device):
             raise ValueError("%s must be int32 with %d dimensions, contiguous, on the pool's device" % (name, dims))
     n_seqs = 0 if lengths is None else len(lengths)
     if page_table is not None and len(page_table) != n_seqs or cu_new is not None and len(cu_new) != n_seqs + 1:

@@ -188,3 +188,15 @@ def test_a_compaction_whose_copies_fail_moves_nothing(monkeypatch):
     assert c.compact() == 2 and made == [[3, 0, 16], [4, 1, 16]] and c.rows[b][:2].tolist() == [0, 1]
     with pytest.raises(RuntimeError):
         c._cache(0)
+
+
+def test_a_step_of_no_sequences_is_one_without_rows():
+    c = _cache()
+    c.step([], [])
+    q, kv = torch.zeros(0, 4, 128, dtype=torch.bfloat16), torch.zeros(0, 2, 128, dtype=torch.bfloat16)
+    assert c.append(0, None, None, q, kv, kv) is q and c.attend(0, q).shape == (0, 4, 128)
+    # a size of one, or of none, may have any stride
+    pool = torch.zeros(4, 2, 16, 128)
+    ints = torch.zeros(6, dtype=torch.int32)
+    assert paged.cache_for(pool, pool.clone(), ints[::3].view(2, 1)[:1], ints[::2][:1]).n_seqs == 1
+    assert paged.cache_for(pool, pool.clone(), ints[::3].view(2, 1), ints[:2]).table_stride == 3
