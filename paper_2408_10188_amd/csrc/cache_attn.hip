@@ -159,6 +159,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
   constexpr int kKL = kD * kElt / 64;                   // 16-byte pieces of a K row that a lane holds
   constexpr int kVC = kD * kElt / 256;                  // .. of a V row
   constexpr int kAcc = kD / 16;                         // O^T accumulators of 16 rows of d
+  // f32: a score is added up as several sums, since each rounds at the size it has grown to.  Its rms error, products of size 1, in units of 2^-24: one sum of 128 products 38.8, two 28.4,
+  // four 21.7; of 64, 19.6 / 14.5 / 11.6.  (Four with two tiles of rows of d = 128: 2 VGPRs spilled, 748 instead of 741 us for 16 x 20000 keys of 28/4 heads and five tokens.)
+  constexpr int kSums = kNT == 2 && kD == 128 ? 2 : 4;
   constexpr int kParts = kNT == 1 ? 3 : 2;              // bf16 numbers that a weight is given to the matrix instructions as
   constexpr int kHalf = kKeys * kD * kElt, kCopies = kHalf / 1024;   // bytes of a step's K (or V), copies that bring them
   // A wavefront's K and V of a step; when a segment ends, the wavefronts' O for kAtOnce tiles of 16 rows, [kAtOnce][kWaves][16][kD] floats, each row's pieces of 4 in
@@ -421,14 +424,23 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
           f32x4 s = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (kBf16) {
 #pragma unroll
-          for (int i = 0; i < kKL; ++i) {
-            if constexpr (kBf16) {
-              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[b][i]), __builtin_bit_cast(bf16x8, qj[i]), s, 0, 0, 0);
-            } else {
+            for (int i = 0; i < kKL; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[b][i]), __builtin_bit_cast(bf16x8, qj[i]), s, 0, 0, 0);
+          } else {
+            f32x4 part[kSums];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[b][i][e]), __uint_as_float(qj[i][e]), s, 0, 0, 0);
-            }
+            for (int y = 0; y < kSums; ++y) part[y] = s;
+#pragma unroll
+            for (int i = 0; i < kKL; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                part[e % kSums] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[b][i][e]), __uint_as_float(qj[i][e]), part[e % kSums], 0, 0, 0);
+#pragma unroll
+            for (int n = kSums / 2; n > 0; n /= 2)
+#pragma unroll
+              for (int y = 0; y < n; ++y) part[y] += part[y + n];
+            s = part[0];
           }
           if (!whole) {
 #pragma unroll

@@ -58,3 +58,20 @@ def test_weights_of_one_new_token_keep_their_bits():
     got = o.double().cpu().numpy().reshape(want.shape)
     err = np.abs(got / want - 1).max()
     assert err <= 2.0 ** -18, err
+
+
+@pytest.mark.parametrize("d,hq,sums", [(64, 8, 4), (64, 40, 4), (128, 8, 4), (128, 40, 2)])
+def test_scores_in_fp32_are_added_up_in_several_sums(d, hq, sums):
+    """One key: LSE is the score, a sum of d products of variance 1.  Of a number x the rounding is uniform within 2^-24 |x| at most, variance x^2 / 3 in units of 2^-24.  In each of the sums, of
+    m = d / sums products, the k-th rounds at variance k: m (m + 1) / 6.  Adding the sums up in pairs rounds at variances 2 m (and then, of four, 4 m).  LSE is twice a
+    product of the score, d / 3 each, with log2 e (off by 0.22 units) and with ln 2 (0.05): d (2 / 3 + 0.05) together.  One sum alone, of variance
+    d (d + 1) / 6, is measured at 38.8 units for d = 128 and at 19.6 for d = 64, above the bounds for four."""
+    seqs, hkv = 800, 2
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    q, k = torch.randn(seqs, hq, d, device=DEV, generator=gen), torch.randn(seqs, hkv, 1, d, device=DEV, generator=gen)
+    _, lse = run(q, k, k, [1] * seqs, 1.0)
+    want = (q.double().view(seqs, hkv, hq // hkv, d) * k.double()).sum(-1).view(seqs, hq).T
+    rms = float((lse.double() - want).pow(2).mean().sqrt()) * 2 ** 24
+    m = d / sums
+    variance = sums * m * (m + 1) / 6 + (2 * 2 * m + 4 * m if sums == 4 else 2 * m) / 3 + d * (2 / 3 + 0.05)
+    assert rms <= math.sqrt(variance), (rms, math.sqrt(variance))
