@@ -264,15 +264,33 @@ def mmsp_rotary_plan(head_dim, theta, sections):
     return rotary
 
 
+def _positions(rotary, n_rows, positions, pos_stride):
+    """Of a tensor, that it is what the kernel will read: int32, on a GPU, with a position for every row on every axis."""
+    if positions is None or isinstance(positions, int):
+        return
+    if str(positions.dtype) != "torch.int32" or not positions.is_cuda:
+        raise ValueError("positions must be int32 on the GPU, not %s on %s" % (positions.dtype, positions.device))
+    last = (rotary.n_axes - 1) * pos_stride + n_rows
+    if last > positions.numel() and last > positions.untyped_storage().nbytes() // 4 - positions.storage_offset():
+        raise ValueError("positions of %d elements are too few for %d rows on %d axes" % (positions.numel(), n_rows, rotary.n_axes))
+
+
 def mmsp_rotary_apply(rotary, n_rows, positions, pos_stride, x, y, inverse=False, stream=0):
     """x, y: one or two MmspHeads each."""
     if len(x) != len(y):
         raise ValueError("%d tensors to turn, %d to write" % (len(x), len(y)))
+    for h in (*x, *y):
+        of = getattr(h, "of", None)                       # of a tensor: its rows and head_dim, and whether it is on a GPU
+        if of is not None and (n_rows > of[0] or rotary.head_dim > of[1] or not of[2]):
+            raise ValueError("%d rows of head_dim %d on the GPU are wanted, not %d of %d%s" % (n_rows, rotary.head_dim, of[0], of[1], "" if of[2] else " elsewhere"))
+    _positions(rotary, n_rows, positions, pos_stride)
     _check(_lib.mmsp_rotary_apply(ctypes.byref(rotary), n_rows, _ptr(positions), pos_stride, len(x), (MmspHeads * len(x))(*x),
                                   (MmspHeads * len(y))(*y), int(inverse), stream or None))
 
 
 def mmsp_cache_append(shape, cache, rotary, positions, pos_stride, q, k, v, q_out=None, stream=0):
+    if rotary is not None:
+        _positions(rotary, cache.n_rows, positions, pos_stride)
     _check(_lib.mmsp_cache_append(ctypes.byref(shape), ctypes.byref(cache), None if rotary is None else ctypes.byref(rotary), _ptr(positions),
                                   pos_stride, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), stream or None))
 

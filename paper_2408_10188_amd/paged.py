@@ -21,7 +21,9 @@ def heads_of(t):
     """mmsp_heads of a tensor [rows, n_heads, d]."""
     if t.dim() != 3 or t.stride(2) != 1:
         raise ValueError("[rows, n_heads, d] with d contiguous is wanted")
-    return B.make_heads(t, t.shape[1], _io(t), *_strides(t))
+    h = B.make_heads(t, t.shape[1], _io(t), *_strides(t))
+    h.of = t.shape[0], t.shape[2], t.is_cuda              # the calls check them
+    return h
 
 
 def shape_for(k_pool, io_dtype, n_q_heads=None, n_rows=0, scale=1.0):

@@ -200,3 +200,36 @@ def test_a_step_of_no_sequences_is_one_without_rows():
     ints = torch.zeros(6, dtype=torch.int32)
     assert paged.cache_for(pool, pool.clone(), ints[::3].view(2, 1)[:1], ints[::2][:1]).n_seqs == 1
     assert paged.cache_for(pool, pool.clone(), ints[::3].view(2, 1), ints[:2]).table_stride == 3
+
+
+class _OnGpu:
+    """What the binding asks of a tensor of positions, as if it lay on a GPU."""
+
+    def __init__(self, t):
+        self.t, self.is_cuda = t, True
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def test_rotary_calls_refuse_tensors_that_are_not_what_the_kernel_reads():
+    """Positions of another type or elsewhere, or too few; Q and K elsewhere, of fewer rows or a smaller head.  (All would be read as they lie.)"""
+    rot = B.mmsp_rotary_plan(128, 1e6, [16, 24, 24])
+    fake = lambda: B.make_heads(4096, 4, B.MMSP_BF16, 512, 128)
+    pos = torch.zeros(3, 5, dtype=torch.int32)
+    shape = B.make_shape(4, 2, 128, B.MMSP_BF16, 0.1, (512, 128), (256, 128), 5)
+    cache = B.make_cache(4096, 4096, (4096, 128, 2048), 9, 16, 4096, 4, 4, 5, 4096, None, 5)
+    for p, stride in ((pos, 5), (_OnGpu(pos.long()), 5), (_OnGpu(pos.float()), 5), (_OnGpu(pos[:2].clone()), 5), (_OnGpu(pos), 6), (_OnGpu(pos[:, 1:]), 5)):
+        with pytest.raises(ValueError):
+            B.mmsp_rotary_apply(rot, 5, p, stride, [fake()], [fake()])
+        with pytest.raises(ValueError):
+            B.mmsp_cache_append(shape, cache, rot, p, stride, 4096, 4096, 4096, 4096)
+    B._positions(rot, 4, _OnGpu(pos[:, 1:]), 5)              # columns of a wider tensor reach to its end
+    B._positions(rot, 5, _OnGpu(pos), 5)
+    on_cpu = paged.heads_of(torch.zeros(5, 4, 128, dtype=torch.bfloat16))
+    few, narrow = fake(), fake()
+    few.of, narrow.of = (4, 128, True), (5, 64, True)
+    for h in (on_cpu, few, narrow):
+        for x, y in ((h, fake()), (fake(), h)):
+            with pytest.raises(ValueError):
+                B.mmsp_rotary_apply(rot, 5, _OnGpu(pos), 5, [fake(), x], [fake(), y])
