@@ -57,12 +57,20 @@ def cache_for(k_pool, v_pool, page_table=None, lengths=None, n_rows=0, cu_new=No
                         cu_new, n_rows, most_new)
 
 
+def _capturing(device):
+    import torch
+    return device.type == "cuda" and torch.cuda.is_current_stream_capturing()
+
+
 class PagedCache:
     """The cache of a model's layers on one GPU: sequences are added, forked, extended and freed; pages are shared by forked
     sequences until one of them writes to its partly filled last page, and moved to the front of the pool on demand.
 
     Everything is enqueued on torch's current stream; calls on other streams are the caller's to order.  `step` says which new
-    tokens come next; `append` and `attend` then run once per layer."""
+    tokens come next; `append` and `attend` then run once per layer.
+
+    None of it can be captured into a graph: a step's tables and workspace are new tensors that go with the next step, and a replay after that would read
+    and write memory that others have by then.  A program that replays its steps keeps arrays of its own and makes the C calls."""
 
     def __init__(self, n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_tokens, dtype, device="cuda"):
         import torch
@@ -72,6 +80,10 @@ class PagedCache:
         self.pages = B.make_pages(self._refs, self._free, page_size)
         self.rows, self.lengths, self._next = {}, {}, 0
         self._step = self._ws = None
+
+    def _eager(self):
+        if _capturing(self.k.device):
+            raise RuntimeError("PagedCache cannot be captured into a graph: its arrays do not outlive a step (capture mmsp_cache_append and mmsp_cache_attn over arrays that stay)")
 
     def _add(self, row, length):
         self._next += 1
@@ -105,6 +117,7 @@ class PagedCache:
 
     def compact(self):
         """Moves the pages in use to the front of the pool; returns how many there are.  Where the copies cannot be made it raises, and no page has moved."""
+        self._eager()
         names = list(self.rows)
         table = np.stack([self.rows[s] for s in names]) if names else np.zeros((0, self.max_pages), dtype=np.int32)
         before = self._refs.copy(), self._free.copy(), self.pages.n_free
@@ -124,6 +137,7 @@ class PagedCache:
         pages for them; raises MmspError (status MMSP_ERR_NO_PAGES) where the pool has too few.  A call that raises, for whatever
         reason, has changed nothing: the step before it is still the present one."""
         import torch
+        self._eager()
         if len(set(seqs)) != len(seqs) or len(seqs) != len(n_new) or min(n_new, default=0) < 0:
             raise ValueError("every sequence once, with a number of new tokens")
         copies, done = [], []
@@ -176,6 +190,7 @@ class PagedCache:
         """Writes the step's K (turned by `rotary` at `positions` [n_axes, rows]) and V into `layer`'s pages; returns Q turned (into q_out:
         contiguous, or q itself, which is also what None means)."""
         import torch
+        self._eager()
         cache, n = self._cache(layer), self._step[3]
         q_out = q if q_out is None else q_out
         for t in (q, k, v, q_out):
@@ -201,6 +216,7 @@ class PagedCache:
         """Attention of the step's rows over `layer`'s cache: O in q's type (into o_final, made if nothing is given), or the
         partial result (o, lse) for mmsp_attn_merge.  Dense [rows, n_q_heads, d] and [n_q_heads, rows]."""
         import torch
+        self._eager()
         cache, n = self._cache(layer), self._step[3]
         if q.shape != (n, self.n_q_heads, self.k.shape[-1]) or q.dtype != self.k.dtype or q.stride(2) != 1 or q.device != self.k.device:
             raise ValueError("q must be %s [%d, %d, %d] on the pool's device" % (self.k.dtype, n, self.n_q_heads, self.k.shape[-1]))

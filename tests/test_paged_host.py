@@ -233,3 +233,20 @@ def test_rotary_calls_refuse_tensors_that_are_not_what_the_kernel_reads():
         for x, y in ((h, fake()), (fake(), h)):
             with pytest.raises(ValueError):
                 B.mmsp_rotary_apply(rot, 5, _OnGpu(pos), 5, [fake(), x], [fake(), y])
+
+
+def test_calls_under_capture_are_refused(monkeypatch):
+    """A graph would go on reading a step's arrays after the next step has let go of them."""
+    c = _cache()
+    a, b = c.add(), c.add()
+    c.step([a, b], [3, 20])
+    c.free(a)
+    before, step = _state(c), c._step
+    q, kv = torch.zeros(3, 4, 128, dtype=torch.bfloat16), torch.zeros(3, 2, 128, dtype=torch.bfloat16)
+    with monkeypatch.context() as m:
+        m.setattr(paged, "_capturing", lambda device: True)
+        for call in (lambda: c.step([b], [1]), c.compact, lambda: c.append(0, None, None, q, kv, kv), lambda: c.attend(0, q)):
+            with pytest.raises(RuntimeError, match="captured"):
+                call()
+    assert _state(c) == before and c._step is step
+    c.step([b], [1])
