@@ -5,6 +5,7 @@ callers for device memory and streams, never for arithmetic on the attention pat
 There is no fallback: if the library has not been built, importing this module raises.
 """
 import ctypes
+import importlib.util
 import os
 
 import numpy as np
@@ -77,12 +78,18 @@ class MmspError(RuntimeError):
 if not os.path.exists(LIB_PATH):
     raise ImportError("libmmsp.so is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "
                       "(or python paper_2408_10188_amd/build.py) first; there is no fallback path")
-try:
-    # torch brings a HIP runtime of its own, which the library shares if it is there first; loaded the other way round there are two in the
-    # process, and the one behind the library sees no device.
-    import torch  # noqa: F401
-except ImportError:
-    pass
+
+
+def _one_hip_runtime():
+    """torch brings a HIP runtime of its own, which the library shares if it is there first; loaded the other way round there are two in the
+    process, and the one behind the library sees no device.  The runtime alone is loaded here: a program that only plans layouts or pages does not wait for torch."""
+    spec = importlib.util.find_spec("torch")
+    path = os.path.join(os.path.dirname(spec.origin), "lib", "libamdhip64.so") if spec is not None and spec.origin else ""
+    if os.path.exists(path):
+        ctypes.CDLL(path)
+
+
+_one_hip_runtime()
 _lib = ctypes.CDLL(LIB_PATH)
 
 _P, _I64, _I32, _INT, _SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_size_t

@@ -250,3 +250,9 @@ def test_calls_under_capture_are_refused(monkeypatch):
                 call()
     assert _state(c) == before and c._step is step
     c.step([b], [1])
+
+
+def test_the_binding_alone_does_not_import_torch():
+    """A host program that plans layouts or pages does not pay for torch's start."""
+    code = "from paper_2408_10188_amd import binding, paged\nimport sys\nprint('torch' in sys.modules, binding.mmsp_zigzag_layout(64, 4, 0, False)[0])"
+    assert subprocess.run([sys.executable, "-c", code], cwd=ROOT, check=True, capture_output=True, text=True).stdout.split() == ["False", "(0,", "7)"]
