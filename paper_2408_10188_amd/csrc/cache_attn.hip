@@ -58,9 +58,10 @@ __device__ __forceinline__ PairShape pairs_of(const CacheAttnArgs& a, const Team
   return p;
 }
 
-// kN numbers to `at` and on, as bf16 or fp32.
+// kN numbers, 4 or 8, to `at` and on, as bf16 or fp32.
 template <bool kBf16, int kN>
 __device__ __forceinline__ void store_row(void* to, int64_t at, const float (&x)[kN]) {
+  static_assert(kN == 4 || kN == 8, "whole pieces of 4");
   if constexpr (kBf16) {
     uint32_t w[kN / 2];
 #pragma unroll
@@ -71,10 +72,7 @@ __device__ __forceinline__ void store_row(void* to, int64_t at, const float (&x)
   } else {
     float* const p = reinterpret_cast<float*>(to) + at;
 #pragma unroll
-    for (int e = 0; e < kN; e += kN < 4 ? 2 : 4) {
-      if constexpr (kN < 4) *reinterpret_cast<f32x2*>(p + e) = f32x2{x[e], x[e + 1]};
-      else *reinterpret_cast<f32x4*>(p + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-    }
+    for (int e = 0; e < kN; e += 4) *reinterpret_cast<f32x4*>(p + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
   }
 }
 
@@ -653,8 +651,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
             *reinterpret_cast<f32x4*>(red_at(j - j0, wave, col, d)) = f32x4{acc[j][e][i], acc[j][e + 1][i], acc[j][e + 2][i], acc[j][e + 3][i]};
           }
       __syncthreads();
-      constexpr int kShare = kThreads / 16, kEach = kD / kShare, kPiece = kEach < 4 ? kEach : 4;   // threads of a row, elements of each, .. at once
-      typedef __attribute__((__vector_size__(kPiece * sizeof(float)))) float piece_t;
+      constexpr int kShare = kThreads / 16, kEach = kD / kShare;   // threads of a row, elements of each
+      static_assert(kEach == 4 || kEach == 8, "a thread takes whole pieces of 4");
       const int row = tid / kShare, d0 = tid % kShare * kEach;
 #pragma unroll
       for (int j = j0; j < min(j0 + kAtOnce, kNT); ++j) {
@@ -671,10 +669,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a, Tea
           const float f = __builtin_amdgcn_exp2f(red_m[w][jr] - ref);
           sum += f * red_l[w][jr];
 #pragma unroll
-          for (int e = 0; e < kEach; e += kPiece) {
-            const piece_t y = *reinterpret_cast<const piece_t*>(red_at(j - j0, w, row, d0 + e));
+          for (int e = 0; e < kEach; e += 4) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(red_at(j - j0, w, row, d0 + e));
 #pragma unroll
-            for (int k = 0; k < kPiece; ++k) x[e + k] += f * y[k];
+            for (int k = 0; k < 4; ++k) x[e + k] += f * y[k];
           }
         }
         const int i = group0 + jr;
