@@ -313,6 +313,9 @@ def mmsp_cache_attn(shape, cache, q, o_final, o, lse, workspace=None, workspace_
 
 def mmsp_cache_copy_pages(shape, cache, n_layers, layer_stride, copies, n_copies, stream=0):
     """copies: device int32 tensor [n_copies, 3] of (src, dst, n_tokens)."""
+    if copies is not None and not isinstance(copies, int) and (str(copies.dtype) != "torch.int32" or not copies.is_cuda or not copies.is_contiguous()
+                                                              or copies.numel() < 3 * n_copies):
+        raise ValueError("copies must be int32 [%d, 3] on the GPU, contiguous, not %s %s on %s" % (n_copies, copies.dtype, tuple(copies.shape), copies.device))
     _check(_lib.mmsp_cache_copy_pages(ctypes.byref(shape), ctypes.byref(cache), n_layers, layer_stride, _ptr(copies), n_copies, stream or None))
 
 

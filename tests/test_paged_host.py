@@ -256,3 +256,12 @@ def test_the_binding_alone_does_not_import_torch():
     """A host program that plans layouts or pages does not pay for torch's start."""
     code = "from paper_2408_10188_amd import binding, paged\nimport sys\nprint('torch' in sys.modules, binding.mmsp_zigzag_layout(64, 4, 0, False)[0])"
     assert subprocess.run([sys.executable, "-c", code], cwd=ROOT, check=True, capture_output=True, text=True).stdout.split() == ["False", "(0,", "7)"]
+
+
+def test_page_copies_refuse_lists_that_are_not_what_the_kernel_reads():
+    shape, cache = B.make_shape(4, 2, 128, B.MMSP_BF16, 0.1, (512, 128), (256, 128), 5), B.make_cache(4096, 4096, (4096, 128, 2048), 9, 16)
+    copies = torch.zeros(4, 3, dtype=torch.int32)
+    for x, n in ((copies, 4), (_OnGpu(copies.long()), 4), (_OnGpu(copies), 5), (_OnGpu(copies.t()), 4), (_OnGpu(copies[:, :2]), 2)):
+        with pytest.raises(ValueError):
+            B.mmsp_cache_copy_pages(shape, cache, 1, 0, x, n)
+    B.mmsp_cache_copy_pages(shape, cache, 1, 0, _OnGpu(copies), 0)
