@@ -7,6 +7,7 @@ There is no fallback: if the library has not been built, importing this module r
 import ctypes
 import importlib.util
 import os
+import sys
 
 import numpy as np
 
@@ -51,6 +52,7 @@ class MmspRotary(ctypes.Structure):
 class MmspHeads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+    of = None                                             # of a tensor: the rows that a call may have (-1: it is not on a GPU), and its head_dim
 
 
 class MmspCache(ctypes.Structure):
@@ -273,9 +275,9 @@ def mmsp_rotary_plan(head_dim, theta, sections):
 
 def _positions(rotary, n_rows, positions, pos_stride):
     """Of a tensor, that it is what the kernel will read: int32, on a GPU, with a position for every row on every axis."""
-    if positions is None or isinstance(positions, int):
+    if positions is None or positions.__class__ is int:
         return
-    if str(positions.dtype) != "torch.int32" or not positions.is_cuda:
+    if positions.dtype is not sys.modules["torch"].int32 or not positions.is_cuda:
         raise ValueError("positions must be int32 on the GPU, not %s on %s" % (positions.dtype, positions.device))
     last = (rotary.n_axes - 1) * pos_stride + n_rows
     if last > positions.numel() and last > positions.untyped_storage().nbytes() // 4 - positions.storage_offset():
@@ -286,10 +288,11 @@ def mmsp_rotary_apply(rotary, n_rows, positions, pos_stride, x, y, inverse=False
     """x, y: one or two MmspHeads each."""
     if len(x) != len(y):
         raise ValueError("%d tensors to turn, %d to write" % (len(x), len(y)))
+    d = rotary.head_dim
     for h in (*x, *y):
-        of = getattr(h, "of", None)                       # of a tensor: its rows and head_dim, and whether it is on a GPU
-        if of is not None and (n_rows > of[0] or rotary.head_dim > of[1] or not of[2]):
-            raise ValueError("%d rows of head_dim %d on the GPU are wanted, not %d of %d%s" % (n_rows, rotary.head_dim, of[0], of[1], "" if of[2] else " elsewhere"))
+        of = h.of
+        if of is not None and (n_rows > of[0] or d > of[1]):
+            raise ValueError("a tensor on the GPU with %d rows of head_dim %d is wanted, not %s of %d" % (n_rows, d, "%d" % of[0] if of[0] >= 0 else "one elsewhere", of[1]))
     _positions(rotary, n_rows, positions, pos_stride)
     _check(_lib.mmsp_rotary_apply(ctypes.byref(rotary), n_rows, _ptr(positions), pos_stride, len(x), (MmspHeads * len(x))(*x),
                                   (MmspHeads * len(y))(*y), int(inverse), stream or None))
@@ -313,7 +316,7 @@ def mmsp_cache_attn(shape, cache, q, o_final, o, lse, workspace=None, workspace_
 
 def mmsp_cache_copy_pages(shape, cache, n_layers, layer_stride, copies, n_copies, stream=0):
     """copies: device int32 tensor [n_copies, 3] of (src, dst, n_tokens)."""
-    if copies is not None and not isinstance(copies, int) and (str(copies.dtype) != "torch.int32" or not copies.is_cuda or not copies.is_contiguous()
+    if copies is not None and not isinstance(copies, int) and (copies.dtype is not sys.modules["torch"].int32 or not copies.is_cuda or not copies.is_contiguous()
                                                               or copies.numel() < 3 * n_copies):
         raise ValueError("copies must be int32 [%d, 3] on the GPU, contiguous, not %s %s on %s" % (n_copies, copies.dtype, tuple(copies.shape), copies.device))
     _check(_lib.mmsp_cache_copy_pages(ctypes.byref(shape), ctypes.byref(cache), n_layers, layer_stride, _ptr(copies), n_copies, stream or None))

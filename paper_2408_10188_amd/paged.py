@@ -22,7 +22,7 @@ def heads_of(t):
     if t.dim() != 3 or t.stride(2) != 1:
         raise ValueError("[rows, n_heads, d] with d contiguous is wanted")
     h = B.make_heads(t, t.shape[1], _io(t), *_strides(t))
-    h.of = t.shape[0], t.shape[2], t.is_cuda              # the calls check them
+    h.of = t.shape[0] if t.is_cuda else -1, t.shape[2]    # the calls check them
     return h
 
 
