@@ -351,7 +351,8 @@ size_t mmsp_cache_workspace_bytes(const mmsp_shape* shape, const mmsp_cache* cac
  * q: [n_rows, n_q_heads, d] with the shape's q strides (its kv strides are not used).  Results, each may be NULL, not
  * all: o_final dense [n_rows, n_q_heads, d] in io_dtype; o the same in f32, for mmsp_attn_merge; lse
  * [n_q_heads][lse_head_stride]; they do not overlap the inputs.  Meant for one or a few new tokens per sequence (any number is right; a
- * whole prompt is faster through mmsp_attn_step_fwd).  UNSUPPORTED where n_rows * n_q_heads exceeds 2^23, or
+ * whole prompt is faster through mmsp_attn_step_fwd, with Q and K turned by mmsp_rotary_apply; mmsp_cache_append then takes them with
+ * rotary == NULL).  UNSUPPORTED where n_rows * n_q_heads exceeds 2^23, or
  * sequences x KV heads x capacity (max_pages * page_size) some 2^36 tokens.  Results are bit-identical from run to run on one kind of device.
  * With bf16 K and V the weights exp(S_j) are multiplied by V with 24 bits, as in f32, where the layout has groups of 16 rows (16 or fewer rows of a KV head
  * in a sequence: one new token of up to 16 heads a KV head), and with 16 bits, off by up to 2^-17, where there are more; sums and LSE are fp32 in either case.

@@ -17,8 +17,9 @@
 //
 // Teams.  Where a sequence has more rows than a group takes, workgroups on one XCD take a group each and read the same keys at the same time (Teams).
 //
-// Measured, 28/4 heads, one token, both launches: 203 tokens 6.9 us (a chain: lengths, pages and Q, K and V, the results), 256K tokens 87 us, of which the loop reads
-// 6.9 TB/s (a plain read of that size 7.1), 64 sequences of 150 to 16384 tokens 64.4 us.
+// Measured, 28/4 heads, one token, both launches: 203 tokens 7.2 us (a chain: lengths, pages and Q, K and V, the results), 256K tokens 87 us, of which the loop reads
+// 6.9 TB/s (a plain read of that size 7.1), 64 sequences of 150 to 16384 tokens 63.8 us.  The compiler keeps 66 to 97 scalars of a kernel in lanes of vector registers (no vector
+// register goes to memory); what that costs has not been measured.
 #include <algorithm>
 #include <type_traits>
 
@@ -115,6 +116,7 @@ __device__ __forceinline__ Cut usual_cut(int fewest, const Teams& teams) { retur
 //   alone   one tile a workgroup, one workgroup a CU,
 //   split   ranges of several of the smallest tiles, one workgroup a CU (teams of several: two; one costs those with idle members up to 15 %),
 //   shared  one tile a workgroup, two a CU, which get in each other's way (9/8).
+// (The numbers here, in usual_cut and in plan_of are of 28/4 heads in bf16 unless they say otherwise; the rules count keys, rows and CUs, but other heads and f32 have not been measured against them.)
 // 28/4 heads, us with tiles of 128 / 256 / 512 / 1024 keys for two workgroups a CU, and so picked: 20000 keys and three new tokens 20.1 / 20.0 / 17.6 / 22.4, 17.9 (alone);
 // 8 sequences of 5003 and three 28.4 / 27.6 / 27.6 / 24.1, 23.9 (split); 16 of 5003 and five 40.5 / 45.4 / 47.6 / 47.3, 39.8 (split); 64 of 150 to 16384 and one
 // 66.8 / 67.1 / 65.7 / -, 64.6 (split; pairs without extra tiles 67.6); 33 of 100 to 3000 and up to six 29.6 / 24.4 / 28.0 / 28.8, 25.3 (shared).
