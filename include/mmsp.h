@@ -346,7 +346,7 @@ size_t mmsp_cache_workspace_bytes(const mmsp_shape* shape, const mmsp_cache* cac
  * and query head
  *   S_j = softmax_scale * Q . K[token j]  over the tokens j <= the row's own whose page is in this pool,
  *   LSE = ln sum_j exp(S_j),  O = sum_j exp(S_j - LSE) V[token j].
- * A row that sees nothing, or only scores of -inf, gets O = 0, LSE = -inf; one with a NaN or +inf among its scores gets NaNs.  What lies in masked slots,
+ * A row that sees nothing, or only scores of -inf (and finite V), gets O = 0, LSE = -inf; one with a NaN or +inf among its scores gets NaNs.  What lies in masked slots,
  * NaN or infinity included, has no influence.  A NaN in a V that a row sees gives a NaN in that element of O, an infinity gives an infinity or a NaN there.
  * q: [n_rows, n_q_heads, d] with the shape's q strides (its kv strides are not used).  Results, each may be NULL, not
  * all: o_final dense [n_rows, n_q_heads, d] in io_dtype; o the same in f32, for mmsp_attn_merge; lse
